@@ -481,6 +481,56 @@ int srm_k_select(srm_model* m, int64_t R, const float* d_logits, const srm_sampl
 int srm_k_prefill_mixer(srm_model* m, int32_t layer, int64_t Bp, int32_t n, const int32_t* d_tok,
                         float* d_x, void* d_S, void* d_a, uint32_t* d_status, void* stream);
 
+/* ---- matrices in 8 bits, and sampling with parameters per row ------------------------------- *
+ * Operators without a model handle: all arrays are the caller's device memory, of the device that is current, and all
+ * strides count elements. A matrix in 8 bits is rows of e4m3 codes with an fp32 scale per block of 128 columns (the
+ * last block of a row may be shorter), of one row (activations) or of 128 rows (weights): an element stands for its
+ * code's value times its block's scale. Scale (i, b) of a matrix lies at d_scale[i * scale_row + b * scale_blk], i
+ * counting rows or blocks of 128 rows; the strides are free (columns one after the other, scale_blk the larger one,
+ * are the faster order). Widths are multiples of 16; matrices that are not results of srm_k_gemm_fp8 start on 16-byte
+ * boundaries, as do their rows (SRM_ERR_ALIGNMENT). R == 0 or M == 0 does nothing. The calls allocate nothing and can
+ * be captured into a graph; nothing outlives a call. All are asynchronous on `stream`. */
+
+/* RMS norm with the residual's addition, into 8 bits [the norms in front of the feed-forward block and the LM head]:
+ *   h = x + delta, rounded to x's type (d_delta NULL: h = x);  y = h / sqrt(mean(h^2) + eps) * g;
+ *   per row and block of 128 channels: s = max(amax |y| / 448, 2^-100), q = e4m3(y / s), to nearest even.
+ * d_x, d_delta [R, d] each in SRM_DTYPE_FP32, _BF16 or _FP16; d_g float[d]; d_sum [R, d] in x's type takes h (NULL: not
+ * stored; may be d_x itself, with the same stride); d_q uint8[R, d]; scales as above. Squares and their sum are fp32: values
+ * up to 1e17 in magnitude. A row that holds a NaN or an infinity gets codes and scales that are none. d <= 16384, a
+ * multiple of 16 (SRM_ERR_UNSUPPORTED). */
+int srm_k_rms_norm_fp8(int64_t R, int32_t d, const void* d_x, int32_t x_dtype, int64_t x_stride, const void* d_delta,
+                       int32_t delta_dtype, int64_t delta_stride, const float* d_g, float eps, void* d_sum, int64_t sum_stride,
+                       uint8_t* d_q, int64_t q_stride, float* d_scale, int64_t scale_row, int64_t scale_blk, void* stream);
+/* A matrix [R, K] in SRM_DTYPE_FP32, _BF16 or _FP16 into 8 bits: s = max(amax |x| / 448, 2^-100) per block of
+ * block_rows (1 or 128) x 128, q = e4m3(x / s), to nearest even. K a multiple of 16. */
+int srm_k_quant_fp8(int64_t R, int64_t K, const void* d_x, int32_t x_dtype, int64_t x_stride, int32_t block_rows, uint8_t* d_q,
+                    int64_t q_stride, float* d_scale, int64_t scale_row, int64_t scale_blk, void* stream);
+/* Dense projection in 8 bits, D[M, N] = A[M, K] W[N, K]^T (+ bias[n]) (+ what D holds, with accumulate = 1):
+ *   D[m, n] = sum_b sa[m, b] sw[n / 128, b] sum_{k in block b} a[m, k] w[n, k]
+ * d_A uint8[M, K] with a scale per row and block (as the two calls above leave it), d_W uint8[N, K] with a scale per
+ * 128 x 128 block; a block's sum and the sum over the blocks are fp32. d_out in SRM_DTYPE_FP32 or SRM_DTYPE_BF16 (not with
+ * accumulate), rows out_stride apart, aligned to its elements. d_bias float[N] or NULL. d_status (may be NULL): a device
+ * word, SRM_STATUS_WAIT_TIMEOUT. A result does not depend on which other rows are computed with it beyond its last bits (the
+ * order in which the blocks are added). */
+int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t a_stride, const float* d_sa, int64_t sa_row,
+                   int64_t sa_blk, const uint8_t* d_W, int64_t w_stride, const float* d_sw, int64_t sw_row, int64_t sw_blk,
+                   const float* d_bias, int32_t accumulate, void* d_out, int32_t out_dtype, int64_t out_stride, uint32_t* d_status,
+                   void* stream);
+/* Token selection with parameters per row and given random numbers (srm_k_select: one rule for all rows, its own Philox
+ * draws). Row r of d_logits [R, V] (SRM_DTYPE_FP32, _BF16 or _FP16, rows logits_stride apart, aligned to its elements),
+ * with w_i = exp((l_i - l_max) / temperature) and the order (logit descending, id ascending):
+ *   the first top_k of the order (top_k <= 0: all); of these the shortest prefix whose mass reaches top_p times theirs
+ *   (top_p >= 1: all; at least one token); of these the tokens with w_i >= min_p (min_p <= 0: all; l_max always stays);
+ *   d_tok[r] = the lowest id i for which the mass of the kept ids <= i exceeds u times the mass kept, 0 <= u < 1.
+ * d_temperature, d_top_p, d_min_p float[R], d_top_k int32[R], each may be NULL (1, no limit); a temperature below 2^-100
+ * selects greedily (lowest id among the maxima). A NaN parameter has no effect (a NaN temperature: greedy; a NaN u: 0).
+ * The borders are decided as in 64-bit arithmetic, whatever the number of tokens. Minus infinity masks a token, and so does a
+ * NaN; plus infinity takes all of the mass. A NaN or plus infinity, and a row that leaves no token, raise
+ * SRM_STATUS_NONFINITE in *d_status (may be NULL); the latter gets id 0. V <= 262144 (SRM_ERR_UNSUPPORTED). */
+int srm_k_sample(int64_t R, int32_t V, const void* d_logits, int32_t logits_dtype, int64_t logits_stride, const float* d_u,
+                 const float* d_temperature, const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, int32_t* d_tok,
+                 uint32_t* d_status, void* stream);
+
 /* Failure-detection check without a fault: launches one thread that waits, with the bounded wait all pipelines of
  * this library use, on a barrier that nothing completes. After limit_cycles (1 .. 2^31 SM clock cycles) the wait
  * gives up, SRM_STATUS_WAIT_TIMEOUT is raised in *d_status, *d_gave_up (may be NULL) is set to 1 and the kernel ends;

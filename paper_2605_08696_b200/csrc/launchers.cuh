@@ -8,23 +8,6 @@
 namespace {
 
 // ---- kernel launchers -------------------------------------------------------------------------
-// Every other kernel than those of launch_resident_kernel and SmallLaunch goes through here: programmatic stream serialization lets the next kernel's blocks be
-// scheduled and run their set-up while this one drains; each kernel orders itself with pdl_wait().
-template <typename... KArgs, typename... Args>
-cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
-}
-
 // For a kernel whose CTAs wait for one another (a cooperative launch): all of them become resident together whatever else runs
 // on the device. Without it two such kernels from streams of different priority each held SMs that the other waited for, until
 // their bounded waits gave up. Every such kernel goes through here (or SmallLaunch), except the chunk mixers, whose blocks wait

@@ -1,0 +1,136 @@
+// C ABI of the 8-bit operators and of the sampler with parameters per row (see include/srm.h for the contract): argument
+// checking and launches.
+#include "host.cuh"
+
+#include "gemm8.cuh"
+#include "quant8.cuh"
+#include "sample.cuh"
+
+using namespace srm;
+
+namespace {
+
+bool dtype_ok(int t) { return t == SRM_DTYPE_FP32 || t == SRM_DTYPE_BF16 || t == SRM_DTYPE_FP16; }
+int64_t dtype_bytes(int t) { return t == SRM_DTYPE_FP32 ? 4 : 2; }
+
+// f(T{}) with the element type of an SRM_DTYPE_* code
+template <typename F>
+int with_type(int t, F&& f) {
+  return t == SRM_DTYPE_BF16 ? f(bf16{}) : t == SRM_DTYPE_FP16 ? f(fp16{}) : f(float{});
+}
+
+// Rows of `cols` elements that are read or written 16 bytes at a time: base and pitch on 16-byte boundaries, rows not overlapping.
+int rows_ok(const void* p, int64_t rows, int64_t cols, int64_t stride, int64_t elem) {
+  if (p == nullptr || (rows > 1 && stride < cols)) return SRM_ERR_INVALID_ARG;
+  if (!aligned(p, 16) || (rows > 1 && stride * elem % 16)) return SRM_ERR_ALIGNMENT;
+  return SRM_OK;
+}
+int floats_ok(const void* p) { return p == nullptr ? SRM_ERR_INVALID_ARG : !aligned(p, 4) ? SRM_ERR_ALIGNMENT : SRM_OK; }
+// Scales of a matrix: any positive strides.
+int scales_ok(const float* p, int64_t row, int64_t blk) { return row < 1 || blk < 1 ? SRM_ERR_INVALID_ARG : floats_ok(p); }
+
+constexpr int64_t kMaxGrid = 0x7fffffff;
+
+template <typename XT, typename DT>
+int launch_norm(const q8::NormArgs& p, cudaStream_t st) {
+  const int n4 = p.d / 4;
+  const dim3 grid((unsigned)p.R);
+  auto threads = [&](int nv) { return dim3((unsigned)((n4 + nv * 32 - 1) / (nv * 32) * 32)); };
+  ++g_kernel_launches;
+  if (n4 <= 256) SRM_CUDA(launch_kernel(q8::rms_norm_fp8_kernel<1, XT, DT>, grid, threads(1), 0, st, p));
+  else if (n4 <= 1024) SRM_CUDA(launch_kernel(q8::rms_norm_fp8_kernel<2, XT, DT>, grid, threads(2), 0, st, p));
+  else SRM_CUDA(launch_kernel(q8::rms_norm_fp8_kernel<4, XT, DT>, grid, threads(4), 0, st, p));
+  return SRM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int srm_k_rms_norm_fp8(int64_t R, int32_t d, const void* d_x, int32_t x_dtype, int64_t x_stride, const void* d_delta,
+                       int32_t delta_dtype, int64_t delta_stride, const float* d_g, float eps, void* d_sum, int64_t sum_stride,
+                       uint8_t* d_q, int64_t q_stride, float* d_scale, int64_t scale_row, int64_t scale_blk, void* stream) {
+  if (R < 0 || d < 1 || !dtype_ok(x_dtype) || !(eps >= 0.f)) return SRM_ERR_INVALID_ARG;
+  if (d_delta != nullptr && !dtype_ok(delta_dtype)) return SRM_ERR_INVALID_ARG;
+  if (d_delta == nullptr && d_sum != nullptr) return SRM_ERR_INVALID_ARG;
+  if (d % 16 || d > 16384 || R > kMaxGrid) return SRM_ERR_UNSUPPORTED;
+  if (R == 0) return SRM_OK;
+  int rc;
+  if ((rc = rows_ok(d_x, R, d, x_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
+  if (d_delta != nullptr && (rc = rows_ok(d_delta, R, d, delta_stride, dtype_bytes(delta_dtype))) != SRM_OK) return rc;
+  if (d_sum != nullptr && (rc = rows_ok(d_sum, R, d, sum_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
+  if ((rc = rows_ok(d_q, R, d, q_stride, 1)) != SRM_OK) return rc;
+  if ((rc = rows_ok(d_g, 1, d, d, 4)) != SRM_OK) return rc;
+  if ((rc = scales_ok(d_scale, scale_row, scale_blk)) != SRM_OK) return rc;
+  const q8::NormArgs p{R, d, d_x, x_stride, d_delta, delta_stride, d_g, eps, d_sum, sum_stride, d_q, q_stride, d_scale, scale_row, scale_blk};
+  return with_type(x_dtype, [&](auto x) {
+    return with_type(d_delta != nullptr ? delta_dtype : SRM_DTYPE_FP32,
+                     [&](auto dl) { return launch_norm<decltype(x), decltype(dl)>(p, static_cast<cudaStream_t>(stream)); });
+  });
+}
+
+int srm_k_quant_fp8(int64_t R, int64_t K, const void* d_x, int32_t x_dtype, int64_t x_stride, int32_t block_rows, uint8_t* d_q,
+                    int64_t q_stride, float* d_scale, int64_t scale_row, int64_t scale_blk, void* stream) {
+  if (R < 0 || K < 1 || !dtype_ok(x_dtype) || (block_rows != 1 && block_rows != 128)) return SRM_ERR_INVALID_ARG;
+  const int64_t kb = (K + 127) / 128;
+  if (K % 16 || kb > kMaxGrid || R > kMaxGrid) return SRM_ERR_UNSUPPORTED;
+  const int64_t grid = block_rows == 1 ? (R * kb + q8::kQuantThreads / 32 - 1) / (q8::kQuantThreads / 32) : (R + 127) / 128 * kb;
+  if (grid > kMaxGrid) return SRM_ERR_UNSUPPORTED;
+  if (R == 0) return SRM_OK;
+  int rc;
+  if ((rc = rows_ok(d_x, R, K, x_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
+  if ((rc = rows_ok(d_q, R, K, q_stride, 1)) != SRM_OK) return rc;
+  if ((rc = scales_ok(d_scale, scale_row, scale_blk)) != SRM_OK) return rc;
+  const q8::QuantArgs p{R, K, d_x, x_stride, d_q, q_stride, d_scale, scale_row, scale_blk};
+  return with_type(x_dtype, [&](auto x) -> int {
+    using XT = decltype(x);
+    ++g_kernel_launches;
+    SRM_CUDA(launch_kernel(block_rows == 1 ? q8::quant_rows_kernel<XT> : q8::quant_tiles_kernel<XT>, dim3((unsigned)grid),
+                           dim3(q8::kQuantThreads), 0, static_cast<cudaStream_t>(stream), p));
+    return SRM_OK;
+  });
+}
+
+int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t a_stride, const float* d_sa, int64_t sa_row,
+                   int64_t sa_blk, const uint8_t* d_W, int64_t w_stride, const float* d_sw, int64_t sw_row, int64_t sw_blk,
+                   const float* d_bias, int32_t accumulate, void* d_out, int32_t out_dtype, int64_t out_stride, uint32_t* d_status,
+                   void* stream) {
+  if (M < 0 || N < 1 || K < 1 || (accumulate != 0 && accumulate != 1)) return SRM_ERR_INVALID_ARG;
+  if (out_dtype != SRM_DTYPE_FP32 && out_dtype != SRM_DTYPE_BF16) return SRM_ERR_INVALID_ARG;
+  if (K % 16 || K > (1 << 20) || M > (1 << 30) || N > (1 << 30) || (accumulate && out_dtype != SRM_DTYPE_FP32)) return SRM_ERR_UNSUPPORTED;
+  if (M == 0) return SRM_OK;
+  int rc;
+  if ((rc = rows_ok(d_A, M, K, a_stride, 1)) != SRM_OK) return rc;
+  if ((rc = rows_ok(d_W, N, K, w_stride, 1)) != SRM_OK) return rc;
+  if ((rc = scales_ok(d_sa, sa_row, sa_blk)) != SRM_OK || (rc = scales_ok(d_sw, sw_row, sw_blk)) != SRM_OK) return rc;
+  if (d_bias != nullptr && (rc = floats_ok(d_bias)) != SRM_OK) return rc;
+  if (d_out == nullptr || (M > 1 && out_stride < N)) return SRM_ERR_INVALID_ARG;
+  if (!aligned(d_out, (size_t)dtype_bytes(out_dtype))) return SRM_ERR_ALIGNMENT;
+  const g8::Args g{M, N, K, d_A, a_stride, d_sa, sa_row, sa_blk, d_W, w_stride, d_sw, sw_row, sw_blk, d_bias, accumulate, d_out, out_stride, d_status};
+  const dim3 grid((unsigned)((N + 15) / 16), (unsigned)((M + 15) / 16));
+  ++g_kernel_launches;
+  SRM_CUDA(launch_kernel(out_dtype == SRM_DTYPE_FP32 ? g8::gemm8_simple_kernel<float> : g8::gemm8_simple_kernel<bf16>, grid, dim3(256), 0,
+                         static_cast<cudaStream_t>(stream), g));
+  return SRM_OK;
+}
+
+int srm_k_sample(int64_t R, int32_t V, const void* d_logits, int32_t logits_dtype, int64_t logits_stride, const float* d_u,
+                 const float* d_temperature, const int32_t* d_top_k, const float* d_top_p, const float* d_min_p, int32_t* d_tok,
+                 uint32_t* d_status, void* stream) {
+  if (R < 0 || V < 1 || !dtype_ok(logits_dtype)) return SRM_ERR_INVALID_ARG;
+  if (V > 262144 || R > kMaxGrid) return SRM_ERR_UNSUPPORTED;
+  if (R == 0) return SRM_OK;
+  if (d_logits == nullptr || d_u == nullptr || d_tok == nullptr || (R > 1 && logits_stride < V)) return SRM_ERR_INVALID_ARG;
+  if (!aligned(d_logits, (size_t)dtype_bytes(logits_dtype)) || !aligned(d_u, 4) || !aligned(d_temperature, 4) || !aligned(d_top_k, 4) ||
+      !aligned(d_top_p, 4) || !aligned(d_min_p, 4) || !aligned(d_tok, 4) || !aligned(d_status, 4))
+    return SRM_ERR_ALIGNMENT;
+  const smp::Args p{R, V, d_logits, logits_stride, d_u, d_temperature, d_top_k, d_top_p, d_min_p, d_tok, d_status};
+  return with_type(logits_dtype, [&](auto t) -> int {
+    ++g_kernel_launches;
+    SRM_CUDA(launch_kernel(smp::sample_simple_kernel<decltype(t)>, dim3((unsigned)R), dim3(smp::kSimpleThreads), 0,
+                           static_cast<cudaStream_t>(stream), p));
+    return SRM_OK;
+  });
+}
+
+}  // extern "C"

@@ -2,18 +2,12 @@
 // and state handles, the launch counter / CUDA-event profiler, and the carving of the caller's workspace.
 // Included by srm_api.cu only (one translation unit).
 #pragma once
-#include "../../include/srm.h"
+#include "host.cuh"
 
-#include <cuda.h>
-#include <cuda_runtime.h>
-
-#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
-#include <mutex>
 #include <new>
-#include <utility>
 #include <vector>
 
 #include "common.cuh"
@@ -40,20 +34,6 @@
 using namespace srm;
 
 namespace {
-
-int g_last_cuda_error = 0;
-
-#define SRM_CUDA(expr)                                  \
-  do {                                                  \
-    cudaError_t e__ = (expr);                           \
-    if (e__ != cudaSuccess) {                           \
-      g_last_cuda_error = (int)e__;                     \
-      return SRM_ERR_CUDA;                              \
-    }                                                   \
-  } while (0)
-
-inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 struct Slot { size_t off = 0, bytes = 0; int elem = 4; };
 
@@ -138,23 +118,6 @@ Layout make_layout(const srm_config& c) {
 }
 
 // ---- TMA descriptors ------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled_fn() {
-  static EncodeTiledFn fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  });
-  return fn;
-}
-
 // Row-major [rows, cols] matrix of 2-byte (bf16) or 4-byte (fp32) elements; the box is 128 bytes of
 // one row (the swizzle span) x box_rows rows. planes > 0: as many such matrices, plane_rows rows apart (a third dimension).
 int make_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows, int elem_bytes, int planes = 0, int64_t plane_rows = 0) {
@@ -203,26 +166,7 @@ int make_tmap_layers(CUtensorMap* map, const void* base, int64_t rows, int64_t c
   return SRM_OK;
 }
 
-// cudaFuncAttributeMaxDynamicSharedMemorySize is a per-device setting: remember which (kernel, device) pairs have
-// it, so that a model on a second device of the process gets it too. Safe from several host threads.
-// large_clusters: also allows clusters of more than eight CTAs.
-int ensure_dynamic_smem(const void* func, int bytes, bool large_clusters = false) {
-  static std::mutex mu;
-  static std::vector<std::pair<const void*, int>> done;      // (kernel, device ordinal)
-  int dev = -1;
-  SRM_CUDA(cudaGetDevice(&dev));
-  std::lock_guard<std::mutex> lock(mu);
-  for (const auto& e : done)
-    if (e.first == func && e.second == dev) return SRM_OK;
-  SRM_CUDA(cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-  if (large_clusters) SRM_CUDA(cudaFuncSetAttribute(func, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-  done.emplace_back(func, dev);
-  return SRM_OK;
-}
-
 struct TmapCacheEntry { const void* base; int64_t rows, cols; int box_rows, elem_bytes; CUtensorMap map; };
-
-std::atomic<unsigned long long> g_kernel_launches{0};     // kernels launched by this library since load (all threads)
 
 struct ProfRecord { cudaEvent_t start, stop; int cls; };
 

@@ -2,6 +2,9 @@
 // host runtime (runtime.cuh: layout, handles, workspace; launchers.cuh: kernel launches and the decode step).
 #include "launchers.cuh"
 
+int srm::g_last_cuda_error = 0;
+std::atomic<unsigned long long> srm::g_kernel_launches{0};
+
 // ================================ C ABI =========================================================
 extern "C" {
 
@@ -571,15 +574,6 @@ int srm_k_mixer_step(srm_model* m, int32_t layer, int32_t t, int64_t R, const in
                                 static_cast<cudaStream_t>(stream));
   return launch_mixer(*m, layer, t, R, d_tok, d_x, d_S, d_a, d_status, static_cast<cudaStream_t>(stream));
 }
-
-namespace {
-int device_sm_count(int* sms) {
-  int dev = 0;
-  SRM_CUDA(cudaGetDevice(&dev));
-  SRM_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
-  return SRM_OK;
-}
-}  // namespace
 
 int srm_k_mixer_combined_step(int64_t R, int32_t d, int32_t n_heads, int32_t t, int32_t n_ctx, const float* d_z,
                               float* d_S_row, float* d_S_col, const float* d_alpha_row, const float* d_alpha_col,
