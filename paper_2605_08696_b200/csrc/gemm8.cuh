@@ -1,20 +1,22 @@
 // 8-bit projection with block scales,
 //   D[m, n] = sum_b sa[m, b] sw[n / 128, b] sum_{k in block b} a[m, k] w[n, k]   (+ bias[n]) (+ what D holds),
-// a and w e4m3, blocks of 128 along K, fp32 accumulation.
+// a and w e4m3, blocks of 128 along K, on the 5th-generation tensor cores (tcgen05.mma.kind::f8f6f4, fp32 accumulators).
+//
+// The scales change from block to block of K, so a block's product (four instructions of K = 32) goes to tensor memory by
+// itself and is added, times its scales, to a sum in the registers of the epilogue warps; tensor memory holds the products of
+// two blocks, so that the warps add one while the tensor pipe computes the next.
 #pragma once
 
-#include <cuda_fp8.h>
-
-#include "common.cuh"
+#include "gemm8_ptx.cuh"
 
 namespace srm {
 namespace g8 {
 
+constexpr int kBK = 128;                         // one block of scales = 128 bytes of a row (the swizzle span)
+
 struct Args {
   int64_t M, N, K;             // K a multiple of 16
-  const uint8_t* A; int64_t a_stride;
   const float* sa; int64_t sa_row, sa_blk;
-  const uint8_t* W; int64_t w_stride;
   const float* sw; int64_t sw_row, sw_blk;
   const float* bias;           // [N] or nullptr
   int accumulate;              // D += (fp32 output only)
@@ -22,41 +24,409 @@ struct Args {
   uint32_t* status;
 };
 
-__device__ __forceinline__ void unpack16(uint4 u, float (&f)[16]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// ---- few rows ------------------------------------------------------------------------------------------------
+// The weights take the side of the 128 accumulator lanes and NT rows of A the columns, so a pass over the weights costs
+// 128 x NT products per 128 x 128 weights however few rows there are. A tile (128 weight rows x NT rows of A) is one cluster:
+// its S CTAs share out the blocks of K, and join their sums through distributed shared memory, each for its part of the
+// columns, in the order of the ranks (so the result is the same every time). What bounds it: the weights' bytes; a CTA keeps
+// kBytesInFlight of them on their way.
+// Warps: 0 loads (TMA), 1 issues the MMAs and owns tensor memory, the others add: warp w reads the lanes 32 (w % 4) .. + 31,
+// with NT = 128 eight of them split the columns.
+template <int NT>
+struct Few {
+  static constexpr int kAddWarps = NT == 128 ? 8 : 4;
+  static constexpr int kCols = NT == 128 ? 64 : NT;                    // columns per adding warp
+  static constexpr int kThreads = 64 + 32 * kAddWarps;
+  static constexpr int kWBytes = 128 * kBK, kABytes = NT * kBK;
+  static constexpr int kStage = kWBytes + kABytes;
+  static constexpr int kStages = NT == 128 ? 3 : NT == 64 ? 4 : 5;     // two CTAs per SM
+  static constexpr int kRing = kStages * kStage;
+  static constexpr int kJoin = 128 * NT * 4;                           // a CTA's sums on their way to the cluster (in the ring)
+  static_assert(kJoin <= kRing, "the sums take the place of the operands");
+  static constexpr int kScale = kAddWarps * 2 * kCols * 4;
+  static constexpr int kBytes = kRing + kScale + 256 + 1024;
+  static constexpr int kTmCols = 2 * NT < 32 ? 32 : 2 * NT;
+};
+
+template <int NT, typename OT>
+__global__ void __launch_bounds__(Few<NT>::kThreads) gemm8_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
+                                                                      const Args g) {
+  using F = Few<NT>;
+  pdl_trigger();
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  float* scale = reinterpret_cast<float*>(smem + F::kRing);            // [warp][2][kCols]
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + F::kRing + F::kScale);
+  uint64_t* empty = full + F::kStages;
+  uint64_t* tfull = empty + F::kStages;
+  uint64_t* tempty = tfull + 2;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(tempty + 2);
+
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int ranks = gridDim.x, rank = blockIdx.x;                      // the cluster is the grid's x dimension
+  const int n0 = blockIdx.y * 128, m0 = blockIdx.z * NT;
+  const int kb_all = (int)((g.K + kBK - 1) / kBK), per = (kb_all + ranks - 1) / ranks;
+  const int kb0 = rank * per, kbn = max(0, min(per, kb_all - kb0));
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F::kStages; ++s) { bar_init(&full[s], 1); bar_init(&empty[s], 1); }
+    for (int a = 0; a < 2; ++a) { bar_init(&tfull[a], 1); bar_init(&tempty[a], F::kAddWarps); }
+    bar_init_fence();
+  }
+  if (warp == 1) tm_alloc<1>(slot, F::kTmCols);
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tm = *slot;
+  pdl_wait();
+
+  float acc[F::kCols];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
-    const float2 v = __half22float2(__half2(h));
-    f[2 * i] = v.x; f[2 * i + 1] = v.y;
+  for (int c = 0; c < F::kCols; ++c) acc[c] = 0.f;
+  const int quad = warp & 3, cg = (warp - 2) >> 2;                      // (adding warps)
+  if (warp == 0) {
+    if (one_lane()) {
+      map_prefetch(&tmA);
+      map_prefetch(&tmW);
+      uint32_t phase = 0;
+      int stage = 0;
+      for (int i = 0; i < kbn; ++i) {
+        if (!bar_wait(&empty[stage], phase ^ 1u, g.status)) { drain_copies(); break; }
+        const uint32_t bar = smem_addr(&full[stage]);
+        bar_expect(bar, F::kStage);
+        tile_load<1>(smem_addr(smem + stage * F::kStage), &tmW, bar, (kb0 + i) * kBK, n0);
+        tile_load<1>(smem_addr(smem + stage * F::kStage + F::kWBytes), &tmA, bar, (kb0 + i) * kBK, m0);
+        if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    if (one_lane()) {
+      uint32_t phase = 0;
+      int stage = 0;
+      for (int i = 0; i < kbn; ++i) {
+        const int buf = i & 1;
+        if (!bar_wait(&tempty[buf], ((i >> 1) & 1) ^ 1u, g.status)) break;
+        if (!bar_wait(&full[stage], phase, g.status)) break;
+        fence_after();
+        const uint64_t dw = tile_desc(smem_addr(smem + stage * F::kStage)), da = tile_desc(smem_addr(smem + stage * F::kStage + F::kWBytes));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mma8<1>(tm + buf * NT, dw + 2 * k, da + 2 * k, mma_desc(128, NT), k != 0);
+        mma_commit<1>(&empty[stage]);
+        mma_commit<1>(&tfull[buf]);
+        if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else {
+    float* sc = scale + (warp - 2) * 2 * F::kCols;
+    const float* sw = g.sw + (int64_t)(n0 >> 7) * g.sw_row + (int64_t)kb0 * g.sw_blk;
+    const float* sa = g.sa + (int64_t)kb0 * g.sa_blk;
+    constexpr int kPer = (F::kCols + 31) / 32;
+    const int64_t last = g.M - 1;
+    int64_t off[kPer];                                                  // this lane's rows of A (beyond the last one: the last)
+    float next[kPer], wnext = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int64_t m = m0 + cg * F::kCols + j * 32 + lane;
+      off[j] = (m < last ? m : last) * g.sa_row;
+      next[j] = kbn > 0 ? sa[off[j]] : 0.f;
+    }
+    if (kbn > 0) wnext = *sw;
+    bool ok = true;
+    for (int i = 0; i < kbn; ++i) {
+      const int buf = i & 1;
+      float* mine = sc + buf * F::kCols;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (j * 32 + lane < F::kCols) mine[j * 32 + lane] = next[j] * wnext;
+      if (i + 1 < kbn) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) next[j] = sa[off[j] + (i + 1) * g.sa_blk];
+        wnext = sw[(i + 1) * g.sw_blk];
+      }
+      __syncwarp();
+      if (!bar_wait(&tfull[buf], (i >> 1) & 1, g.status)) { ok = false; break; }
+      fence_after();
+      const uint32_t t = tm + ((uint32_t)(quad * 32) << 16) + buf * NT + cg * F::kCols;
+#pragma unroll
+      for (int c = 0; c < F::kCols; c += 16) {
+        uint32_t r[16];
+        tm_load16(t + c, r);
+        tm_load_wait();
+        if (c + 16 == F::kCols) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(smem_addr(&tempty[buf]));
+        }
+#pragma unroll
+        for (int q = 0; q < 16; q += 4) {
+          const float4 s = *reinterpret_cast<const float4*>(mine + c + q);
+          acc[c + q] = fmaf(s.x, __uint_as_float(r[q]), acc[c + q]);
+          acc[c + q + 1] = fmaf(s.y, __uint_as_float(r[q + 1]), acc[c + q + 1]);
+          acc[c + q + 2] = fmaf(s.z, __uint_as_float(r[q + 2]), acc[c + q + 2]);
+          acc[c + q + 3] = fmaf(s.w, __uint_as_float(r[q + 3]), acc[c + q + 3]);
+        }
+      }
+    }
+    (void)ok;
+  }
+  // Every block of this CTA has been multiplied: the ring's bytes are free for the sums.
+  const int64_t n = n0 + quad * 32 + lane;
+  OT* out = static_cast<OT*>(g.out);
+  if (ranks == 1) {
+    if (warp >= 2 && n < g.N) {
+      const float b = g.bias != nullptr ? g.bias[n] : 0.f;
+#pragma unroll
+      for (int c = 0; c < F::kCols; ++c) {
+        const int64_t m = m0 + cg * F::kCols + c;
+        if (m < g.M) {
+          OT* o = out + m * g.out_stride + n;
+          float v = acc[c] + b;
+          if (g.accumulate) v += to_float(*o);
+          *o = from_float<OT>(v);
+        }
+      }
+    }
+  } else {
+    float* join = reinterpret_cast<float*>(smem);                       // [column][128 lanes]
+    if (warp >= 2) {
+#pragma unroll
+      for (int c = 0; c < F::kCols; ++c) join[(cg * F::kCols + c) * 128 + quad * 32 + lane] = acc[c];
+    }
+    sync_cluster();
+    const int cols = (int)min((int64_t)NT, g.M - m0);
+    const uint32_t base = smem_addr(join);
+    for (int e = threadIdx.x + rank * F::kThreads; e < cols * 128; e += ranks * F::kThreads) {
+      float v = 0.f;
+      for (int r = 0; r < ranks; ++r) v += peer_load(peer_addr(base + e * 4, r));
+      const int64_t col = n0 + (e & 127), m = m0 + (e >> 7);
+      if (col < g.N) {
+        OT* o = out + m * g.out_stride + col;
+        if (g.bias != nullptr) v += g.bias[col];
+        if (g.accumulate) v += to_float(*o);
+        *o = from_float<OT>(v);
+      }
+    }
+    sync_cluster();                                                     // no CTA leaves while its sums are read
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    tm_free<1>(tm, F::kTmCols);
   }
 }
 
-// One output per thread: every product in fp32, a sum per block of 128.
+// ---- many rows -----------------------------------------------------------------------------------------------
+// A CTA pair owns a 256 x 256 tile (256 rows of A over both CTAs' accumulator lanes, 256 weight rows as two halves of 128
+// columns, each half under one scale per block); persistent, tiles taken round-robin, rows fastest. Per block of K each half is
+// four MMAs (256 x 128 x 32) into one of four accumulators of 128 columns: the warps have the time of three halves to fetch one.
+// Sixteen adding warps per CTA: 32 lanes x 64 columns each, in registers until the tile's last block.
+struct Many {
+  static constexpr int kStages = 5;
+  static constexpr int kABytes = 128 * kBK, kWBytes = 128 * kBK, kHalfBytes = 64 * kBK;      // per CTA and block
+  static constexpr int kStage = kABytes + kWBytes;
+  static constexpr int kAddWarps = 16;
+  static constexpr int kCols = 64;
+  static constexpr int kThreads = 64 + 32 * kAddWarps;
+  static constexpr int kBox = 32 * 128;                                 // staged output of a warp: 32 rows x 128 bytes
+  static constexpr int kBytes = kStages * kStage + kAddWarps * kBox + 256 + 1024;
+};
+
+// 32 rows x 128 bytes of finished output (v: the lane's row) from row `row0`, column `col0` on: through the warp's staging box,
+// whose 16-byte pieces are swizzled as the output's tensor map has them, to the TMA unit; or, where the rows' pitch is no
+// multiple of 16 bytes (no tensor map), row by row with plain stores.
 template <typename OT>
-__global__ void __launch_bounds__(256) gemm8_simple_kernel(const Args g) {
-  pdl_trigger();
-  pdl_wait();
-  const int64_t n = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15), m = (int64_t)blockIdx.y * 16 + (threadIdx.x >> 4);
-  if (m >= g.M || n >= g.N) return;
-  const uint8_t *a = g.A + m * g.a_stride, *w = g.W + n * g.w_stride;
-  float acc = 0.f;
-  for (int64_t b = 0; b * 128 < g.K; ++b) {
-    const int64_t k1 = b * 128 + 128 < g.K ? b * 128 + 128 : g.K;
-    float s = 0.f;
-    for (int64_t k = b * 128; k < k1; k += 16) {
-      float fa[16], fw[16];
-      unpack16(__ldg(reinterpret_cast<const uint4*>(a + k)), fa);
-      unpack16(__ldg(reinterpret_cast<const uint4*>(w + k)), fw);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s = fmaf(fa[i], fw[i], s);
-    }
-    acc = fmaf(g.sa[m * g.sa_row + b * g.sa_blk] * g.sw[n / 128 * g.sw_row + b * g.sw_blk], s, acc);
+__device__ __forceinline__ void put_box(const Args& g, const CUtensorMap* tmD, bool mapped, uint8_t* box, int lane, int64_t row0, int64_t col0,
+                                        const uint32_t (&v)[32]) {
+  if (mapped) {
+    if (one_lane()) stores_wait_read();                                // the box before this one has been read
   }
-  if (g.bias != nullptr) acc += g.bias[n];
-  OT* out = static_cast<OT*>(g.out) + m * g.out_stride + n;
-  if (g.accumulate) acc += to_float(*out);
-  *out = from_float<OT>(acc);
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    *reinterpret_cast<uint4*>(box + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+  if (mapped) {
+    fence_async();
+    __syncwarp();
+    if (one_lane()) {
+      if (sizeof(OT) == 4 && g.accumulate) tile_add(tmD, smem_addr(box), (int)col0, (int)row0);
+      else if (sizeof(OT) == 4) tile_store_streaming(tmD, smem_addr(box), (int)col0, (int)row0);
+      else tile_store(tmD, smem_addr(box), (int)col0, (int)row0);
+      stores_commit();
+    }
+  } else {
+    __syncwarp();
+    constexpr int kWords = 32 / (int)sizeof(OT) * 4;                    // elements of a box row
+    const int rows = (int)min((int64_t)32, g.M - row0);
+    for (int r = 0; r < rows; ++r) {
+      OT* o = static_cast<OT*>(g.out) + (row0 + r) * g.out_stride + col0;
+#pragma unroll
+      for (int e = 0; e < kWords; e += 32) {
+        const int c = e + lane, byte = c * (int)sizeof(OT);
+        const OT x = *reinterpret_cast<const OT*>(box + r * 128 + ((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15)));
+        if (col0 + c < g.N) o[c] = g.accumulate ? from_float<OT>(to_float(x) + to_float(o[c])) : x;
+      }
+    }
+    __syncwarp();
+  }
+}
+
+template <typename OT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Many::kThreads, 1)
+gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmD,
+                  const int mapped, const Args g) {
+  using F = Many;
+  pdl_trigger();
+  extern __shared__ uint8_t raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* boxes = smem + F::kStages * F::kStage;
+  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + F::kAddWarps * F::kBox);      // leader's: both CTAs' copies of a stage
+  uint64_t* empty = full + F::kStages;                                  // per CTA: the stage may be filled again
+  uint64_t* tfull = empty + F::kStages;                                 // per CTA [4]: a half's product is there
+  uint64_t* tempty = tfull + 4;                                         // leader's [4]: both CTAs' warps have fetched it
+  uint32_t* slot = reinterpret_cast<uint32_t*>(tempty + 4);
+
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cta_rank();
+  const int64_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < F::kStages; ++s) { bar_init(&full[s], 2); bar_init(&empty[s], 1); }
+    for (int a = 0; a < 4; ++a) { bar_init(&tfull[a], 1); bar_init(&tempty[a], F::kAddWarps); }
+    bar_init_fence();
+  }
+  if (warp == 1) tm_alloc<2>(slot, 512);
+  fence_before();
+  sync_cluster();
+  fence_after();
+  const uint32_t tm = *slot;
+  pdl_wait();
+
+  const int64_t m_tiles = (g.M + 255) / 256, tiles = m_tiles * ((g.N + 255) / 256);
+  const int kbs = (int)((g.K + kBK - 1) / kBK);
+  if (warp == 0) {
+    if (one_lane()) {
+      map_prefetch(&tmA);
+      map_prefetch(&tmW);
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int64_t q = first; ok && q < tiles; q += step) {
+        const int m0 = (int)(q % m_tiles) * 256 + (int)rank * 128, n0 = (int)(q / m_tiles) * 256 + (int)rank * 64;
+        for (int kb = 0; kb < kbs; ++kb) {
+          if (!bar_wait(&empty[stage], phase ^ 1u, g.status)) { ok = false; break; }
+          const uint32_t bar = peer_addr(smem_addr(&full[stage]), 0), dst = smem_addr(smem + stage * F::kStage);
+          bar_expect(bar, F::kStage);
+          tile_load<2>(dst, &tmA, bar, kb * kBK, m0);
+          tile_load<2>(dst + F::kABytes, &tmW, bar, kb * kBK, n0);
+          tile_load<2>(dst + F::kABytes + F::kHalfBytes, &tmW, bar, kb * kBK, n0 + 128);
+          if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok) drain_copies();
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && one_lane()) {
+      int stage = 0;
+      uint32_t phase = 0, it = 0;
+      bool ok = true;
+      for (int64_t q = first; ok && q < tiles; q += step) {
+        for (int kb = 0; ok && kb < kbs; ++kb, ++it) {
+          if (!bar_wait(&full[stage], phase, g.status)) { ok = false; break; }
+          const uint32_t src = smem_addr(smem + stage * F::kStage);
+          const uint64_t da = tile_desc(src);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int buf = (int)(it & 1u) * 2 + h;
+            if (!bar_wait(&tempty[buf], ((it >> 1) & 1u) ^ 1u, g.status)) { ok = false; break; }
+            fence_after();
+            const uint64_t dw = tile_desc(src + F::kABytes + h * F::kHalfBytes);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma8<2>(tm + buf * 128, da + 2 * k, dw + 2 * k, mma_desc(256, 128), k != 0);
+            if (h == 1) mma_commit<2>(&empty[stage]);
+            mma_commit<2>(&tfull[buf]);
+          }
+          if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else {
+    const int quad = warp & 3, cg = (warp - 2) >> 2, h = cg >> 1;
+    uint8_t* box = boxes + (warp - 2) * F::kBox;
+    const uint32_t drained0 = peer_addr(smem_addr(&tempty[h]), 0);
+    uint32_t it = 0;
+    bool ok = true;
+    if (mapped && lane == 0) map_prefetch(&tmD);
+    for (int64_t q = first; ok && q < tiles; q += step) {
+      const int64_t row0 = (q % m_tiles) * 256 + rank * 128 + quad * 32, nh = (q / m_tiles) * 256 + h * 128;
+      const int64_t col0 = nh + (cg & 1) * 64;
+      const float* sa = g.sa + min(row0 + lane, g.M - 1) * g.sa_row;
+      const float* sw = g.sw + (min(nh, g.N - 1) >> 7) * g.sw_row;
+      float acc[F::kCols];
+#pragma unroll
+      for (int c = 0; c < F::kCols; ++c) acc[c] = 0.f;
+      float sa_next = *sa, sw_next = *sw;
+      for (int kb = 0; kb < kbs; ++kb, ++it) {
+        const float s = sa_next * sw_next;
+        if (kb + 1 < kbs) {
+          sa_next = sa[(kb + 1) * g.sa_blk];
+          sw_next = sw[(kb + 1) * g.sw_blk];
+        }
+        const int buf = (int)(it & 1u) * 2 + h;
+        if (!bar_wait(&tfull[buf], (it >> 1) & 1u, g.status)) { ok = false; break; }
+        fence_after();
+        const uint32_t t = tm + ((uint32_t)(quad * 32) << 16) + buf * 128 + (cg & 1) * 64;
+        uint32_t ra[16], rb[16];
+        tm_load16(t, ra);
+        tm_load_wait();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t (&cur)[16] = (c & 1) ? rb : ra;
+          uint32_t (&nxt)[16] = (c & 1) ? ra : rb;
+          if (c < 3) tm_load16(t + 16 * (c + 1), nxt);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(s, __uint_as_float(cur[j]), acc[16 * c + j]);
+          if (c < 3) tm_load_wait();
+          if (c == 2) {                                                 // everything has left tensor memory
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(drained0 + (uint32_t)(it & 1u) * 16u);
+          }
+        }
+      }
+      if (!ok) break;
+      if (row0 < g.M && col0 < g.N) {
+        if (g.bias != nullptr) {
+#pragma unroll
+          for (int c = 0; c < F::kCols; ++c) acc[c] += col0 + c < g.N ? __ldg(g.bias + col0 + c) : 0.f;
+        }
+        uint32_t v[32];
+        if (sizeof(OT) == 4) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(acc[j]);
+          put_box<OT>(g, &tmD, mapped, box, lane, row0, col0, v);
+          if (col0 + 32 < g.N) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(acc[32 + j]);
+            put_box<OT>(g, &tmD, mapped, box, lane, row0, col0 + 32, v);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(acc[2 * j], acc[2 * j + 1]);
+            v[j] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+          put_box<OT>(g, &tmD, mapped, box, lane, row0, col0, v);
+        }
+      }
+    }
+    if (mapped && one_lane()) stores_wait();                            // the boxes are out before shared memory goes away
+  }
+  fence_before();
+  sync_cluster();                                                       // the leader's MMAs use the peer's memory until here
+  if (warp == 1) {
+    fence_after();
+    tm_free<2>(tm, 512);
+  }
 }
 
 }  // namespace g8

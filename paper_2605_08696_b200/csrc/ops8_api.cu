@@ -43,6 +43,88 @@ int launch_norm(const q8::NormArgs& p, cudaStream_t st) {
   return SRM_OK;
 }
 
+// Tensor map of a row-major matrix, box_rows rows x 128 bytes, 128-byte swizzle. (Boxes may reach beyond the matrix: zeros are
+// read there, nothing is written.)
+int byte_map(CUtensorMap* map, CUtensorMapDataType type, int elem, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) { g_last_cuda_error = (int)cudaErrorNotSupported; return SRM_ERR_CUDA; }
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, pitch[1] = {(cuuint64_t)(stride * elem)};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / elem), (cuuint32_t)box_rows}, one[2] = {1, 1};
+  const CUresult r = fn(map, type, 2, const_cast<void*>(base), dims, pitch, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) { g_last_cuda_error = 10000 + (int)r; return SRM_ERR_CUDA; }
+  return SRM_OK;
+}
+
+// Rows that stand alone may be given any stride; a tensor map wants a pitch that covers the row and is a multiple of 16 bytes.
+int64_t map_stride(int64_t rows, int64_t cols, int64_t stride, int64_t elem) {
+  return rows > 1 ? stride : (cols * elem + 15) / 16 * 16 / elem;
+}
+
+template <int NT, typename OT>
+int launch_few(const g8::Args& g, const uint8_t* A, int64_t a_stride, const uint8_t* W, int64_t w_stride, int ranks, cudaStream_t st) {
+  using F = g8::Few<NT>;
+  const auto kernel = g8::gemm8_few_kernel<NT, OT>;
+  int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), F::kBytes);
+  if (rc != SRM_OK) return rc;
+  CUtensorMap ta, tw;
+  if ((rc = byte_map(&ta, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, g.M, g.K, map_stride(g.M, g.K, a_stride, 1), NT)) != SRM_OK) return rc;
+  if ((rc = byte_map(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, W, g.N, g.K, map_stride(g.N, g.K, w_stride, 1), 128)) != SRM_OK) return rc;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ranks, (unsigned)((g.N + 127) / 128), (unsigned)((g.M + NT - 1) / NT));
+  cfg.blockDim = dim3(F::kThreads);
+  cfg.dynamicSmemBytes = F::kBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)ranks; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  ++g_kernel_launches;
+  SRM_CUDA(cudaLaunchKernelEx(&cfg, kernel, ta, tw, g));
+  return SRM_OK;
+}
+
+template <typename OT>
+int launch_many(const g8::Args& g, const uint8_t* A, int64_t a_stride, const uint8_t* W, int64_t w_stride, int sms, cudaStream_t st) {
+  const auto kernel = g8::gemm8_many_kernel<OT>;
+  int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), g8::Many::kBytes);
+  if (rc != SRM_OK) return rc;
+  CUtensorMap ta, tw, td;
+  if ((rc = byte_map(&ta, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, g.M, g.K, map_stride(g.M, g.K, a_stride, 1), 128)) != SRM_OK) return rc;
+  if ((rc = byte_map(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, W, g.N, g.K, map_stride(g.N, g.K, w_stride, 1), 64)) != SRM_OK) return rc;
+  const int elem = (int)sizeof(OT);
+  const int64_t pitch = map_stride(g.M, g.N, g.out_stride, elem);
+  const int mapped = aligned(g.out, 16) && pitch * elem % 16 == 0;
+  td = ta;
+  if (mapped && (rc = byte_map(&td, elem == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, elem, g.out, g.M, g.N, pitch, 32)) != SRM_OK)
+    return rc;
+  const int64_t tiles = (g.M + 255) / 256 * ((g.N + 255) / 256), pairs = sms / 2;
+  ++g_kernel_launches;
+  SRM_CUDA(launch_kernel(kernel, dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(g8::Many::kThreads), g8::Many::kBytes, st, ta, tw, td, mapped, g));
+  return SRM_OK;
+}
+
+template <typename OT>
+int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const uint8_t* W, int64_t w_stride, cudaStream_t st) {
+  int sms = 0;
+  const int rc = device_sm_count(&sms);
+  if (rc != SRM_OK) return rc;
+  const int64_t n_tiles = (g.N + 127) / 128, kb = (g.K + 127) / 128;
+  if (g.M > 256 && g.N > 128) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
+  const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
+  const int64_t m_tiles = (g.M + nt - 1) / nt;
+  if (n_tiles > 65535 || m_tiles > 65535) return SRM_ERR_UNSUPPORTED;
+  int ranks = 1;                       // as many as give every SM two CTAs
+  while (ranks < 8 && 2 * ranks <= kb && n_tiles * m_tiles * ranks * 2 <= 2 * sms) ranks *= 2;
+  if (nt == 16) return launch_few<16, OT>(g, A, a_stride, W, w_stride, ranks, st);
+  if (nt == 32) return launch_few<32, OT>(g, A, a_stride, W, w_stride, ranks, st);
+  if (nt == 64) return launch_few<64, OT>(g, A, a_stride, W, w_stride, ranks, st);
+  return launch_few<128, OT>(g, A, a_stride, W, w_stride, ranks, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -106,12 +188,10 @@ int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t 
   if (d_bias != nullptr && (rc = floats_ok(d_bias)) != SRM_OK) return rc;
   if (d_out == nullptr || (M > 1 && out_stride < N)) return SRM_ERR_INVALID_ARG;
   if (!aligned(d_out, (size_t)dtype_bytes(out_dtype))) return SRM_ERR_ALIGNMENT;
-  const g8::Args g{M, N, K, d_A, a_stride, d_sa, sa_row, sa_blk, d_W, w_stride, d_sw, sw_row, sw_blk, d_bias, accumulate, d_out, out_stride, d_status};
-  const dim3 grid((unsigned)((N + 15) / 16), (unsigned)((M + 15) / 16));
-  ++g_kernel_launches;
-  SRM_CUDA(launch_kernel(out_dtype == SRM_DTYPE_FP32 ? g8::gemm8_simple_kernel<float> : g8::gemm8_simple_kernel<bf16>, grid, dim3(256), 0,
-                         static_cast<cudaStream_t>(stream), g));
-  return SRM_OK;
+  const g8::Args g{M, N, K, d_sa, sa_row, sa_blk, d_sw, sw_row, sw_blk, d_bias, accumulate, d_out, out_stride, d_status};
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (out_dtype == SRM_DTYPE_FP32) return launch_gemm8<float>(g, d_A, a_stride, d_W, w_stride, st);
+  return launch_gemm8<bf16>(g, d_A, a_stride, d_W, w_stride, st);
 }
 
 int srm_k_sample(int64_t R, int32_t V, const void* d_logits, int32_t logits_dtype, int64_t logits_stride, const float* d_u,
