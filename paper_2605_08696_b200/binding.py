@@ -248,60 +248,70 @@ def k_mixer_kernel_scan(t0, Z, P, alpha, beta, lam, Y):
 # Arguments of another type, shape, device or layout than the docstrings say raise ValueError before anything is launched;
 # what the C call refuses raises SRMError. The kernels run on the tensors' own device, on its current stream.
 
+# Small calls are bound by the host, so this marshalling is kept short: messages are only formed once something is wrong.
+
 _CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_FP16}
+_OUT_CODES = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+_E4M3 = {torch.float8_e4m3fn: 0, torch.uint8: 0}
+_F32, _INT32 = torch.float32, torch.int32
+# the raw handle of a device's current stream, without a Stream object around it (2 us)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
-
-
-def _matrix(t, rows, cols, dtypes, name):
-    """Address and row stride (elements) of a [rows, cols] tensor whose rows are contiguous."""
-    _need(t.dtype in dtypes, f"{name}: {t.dtype} is not supported")
-    _need(t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, f"{name}: shape {tuple(t.shape)}, not ({rows}, {cols})")
-    s = t.stride()
-    _need(cols == 1 or s[1] == 1, f"{name}: the elements of a row must be contiguous")
-    return t.data_ptr(), s[0] if rows > 1 else cols
+def _matrix(t, rows, cols, codes, name):
+    """Address, type code and row stride (elements) of a [rows, cols] tensor whose rows are contiguous."""
+    code = codes.get(t.dtype)
+    if code is None or t.shape != (rows, cols):
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, must be ({rows}, {cols}) of {[str(c) for c in codes]}")
+    s0, s1 = t.stride()
+    if s1 != 1 and cols != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return t.data_ptr(), code, s0
 
 
 def _scales(t, rows, cols, name):
     """Address and strides of a [rows, cols] tensor of block scales, in any order."""
-    _need(t.dtype == torch.float32, f"{name}: {t.dtype}, not float32")
-    _need(t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols, f"{name}: shape {tuple(t.shape)}, not ({rows}, {cols})")
-    s = t.stride()
-    return t.data_ptr(), s[0] if rows > 1 else 1, s[1] if cols > 1 else 1
+    if t.dtype is not _F32 or t.shape != (rows, cols):
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, must be ({rows}, {cols}) float32")
+    s0, s1 = t.stride()
+    return t.data_ptr(), s0, s1
 
 
 def _vector(t, n, dtype, name):
     """Address of a contiguous vector of n elements, or None."""
     if t is None:
         return None
-    _need(t.dtype == dtype and t.dim() == 1 and t.shape[0] == n and (n <= 1 or t.stride(0) == 1),
-          f"{name}: must be a contiguous vector of {n} {dtype}")
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name}: must be a contiguous vector of {n} {dtype}")
     return t.data_ptr()
 
 
 def _status_word(t):
     if t is None:
         return None
-    _need(t.dtype in (torch.int32, torch.uint32) and t.numel() >= 1, "status: must be an int32 tensor")
+    if t.dtype not in (torch.int32, torch.uint32) or t.numel() < 1:
+        raise ValueError("status: must be an int32 tensor")
     return t.data_ptr()
 
 
-_E4M3 = (torch.float8_e4m3fn, torch.uint8)
+def _device_of(first, *others):
+    """The one CUDA device that all the tensors (or None) are on."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("the tensors must be on a CUDA device")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("all tensors must be on one CUDA device")
+    return dev
 
 
-def _call(name, tensors, *args):
-    """The C call on the device that all the tensors are on, and on its current stream."""
-    dev = tensors[0].device
-    for t in tensors:
-        _need(t is None or (t.is_cuda and t.device == dev), f"{name}: all tensors must be on one CUDA device")
-    if dev.index == torch.cuda.current_device():
-        rc = getattr(_lib(), name)(*args, torch.cuda.current_stream().cuda_stream)
+def _run(name, dev, *args):
+    """The C call on device `dev`, on its current stream."""
+    if dev == torch.cuda.current_device():
+        rc = getattr(_LIB or _lib(), name)(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = getattr(_lib(), name)(*args, torch.cuda.current_stream().cuda_stream)
+            rc = getattr(_lib(), name)(*args, _raw_stream(dev))
     if rc != 0:
         raise SRMError(rc, name)
 
@@ -310,58 +320,59 @@ def k_rms_norm_fp8(x, g, q, scales, delta=None, sum_out=None, eps=1e-5):
     """RMS norm of h = x + delta into e4m3 with a scale per row and 128 channels (srm_k_rms_norm_fp8). x, delta [R, d] in fp32,
     bf16 or fp16 (each its own; rows may be strided); g [d] fp32; q [R, d] float8_e4m3fn (or uint8); scales [R, ceil(d / 128)]
     fp32 in any order; sum_out [R, d] in x's type takes h, and may be x. Writes q, scales and sum_out."""
-    _need(x.dim() == 2, "x: must be [R, d]")
     R, d = x.shape
-    xp, xs = _matrix(x, R, d, _CODES, "x")
-    dp, ds = _matrix(delta, R, d, _CODES, "delta") if delta is not None else (None, 0)
-    sp, ss = _matrix(sum_out, R, d, (x.dtype,), "sum_out") if sum_out is not None else (None, 0)
-    qp, qs = _matrix(q, R, d, _E4M3, "q")
+    xp, xc, xs = _matrix(x, R, d, _CODES, "x")
+    dp, dc, ds = _matrix(delta, R, d, _CODES, "delta") if delta is not None else (None, 0, 0)
+    sp, _, ss = _matrix(sum_out, R, d, {x.dtype: 0}, "sum_out") if sum_out is not None else (None, 0, 0)
+    qp, _, qs = _matrix(q, R, d, _E4M3, "q")
     cp, cr, cb = _scales(scales, R, (d + 127) // 128, "scales")
-    _call("srm_k_rms_norm_fp8", (x, g, q, scales, delta, sum_out), R, d, xp, _CODES[x.dtype], xs, dp,
-          _CODES[delta.dtype] if delta is not None else 0, ds, _vector(g, d, torch.float32, "g"), eps, sp, ss, qp, qs, cp, cr, cb)
+    gp = _vector(g, d, _F32, "g")
+    _run("srm_k_rms_norm_fp8", _device_of(x, g, q, scales, delta, sum_out), R, d, xp, xc, xs, dp, dc, ds, gp, eps, sp, ss, qp, qs,
+         cp, cr, cb)
 
 
 def k_quant_fp8(x, q, scales, block_rows=1):
     """x [R, K] (fp32, bf16 or fp16, rows may be strided) into e4m3 with a scale per block of block_rows (1: activations, 128:
     weights) x 128 (srm_k_quant_fp8). q [R, K] float8_e4m3fn (or uint8); scales [ceil(R / block_rows), ceil(K / 128)] fp32 in
     any order. Writes q and scales."""
-    _need(x.dim() == 2, "x: must be [R, K]")
-    _need(block_rows in (1, 128), "block_rows: 1 or 128")
+    if block_rows != 1 and block_rows != 128:
+        raise ValueError("block_rows: 1 or 128")
     R, K = x.shape
-    xp, xs = _matrix(x, R, K, _CODES, "x")
-    qp, qs = _matrix(q, R, K, _E4M3, "q")
+    xp, xc, xs = _matrix(x, R, K, _CODES, "x")
+    qp, _, qs = _matrix(q, R, K, _E4M3, "q")
     cp, cr, cb = _scales(scales, -(-R // block_rows), (K + 127) // 128, "scales")
-    _call("srm_k_quant_fp8", (x, q, scales), R, K, xp, _CODES[x.dtype], xs, block_rows, qp, qs, cp, cr, cb)
+    _run("srm_k_quant_fp8", _device_of(x, q, scales), R, K, xp, xc, xs, block_rows, qp, qs, cp, cr, cb)
 
 
 def k_gemm_fp8(a, a_scales, w, w_scales, out, bias=None, accumulate=False, status=None):
     """out = a w^T (+ bias) (+ out, with accumulate: fp32 only) of two matrices in 8 bits (srm_k_gemm_fp8): a [M, K] with
     a_scales [M, ceil(K / 128)], w [N, K] with w_scales [ceil(N / 128), ceil(K / 128)], e4m3 (or uint8) and fp32 in any order;
     out [M, N] fp32 or bf16 (rows may be strided); bias [N] fp32. Writes out."""
-    _need(a.dim() == 2 and w.dim() == 2, "a, w: must be matrices")
-    (M, K), N = a.shape, w.shape[0]
+    M, K = a.shape
+    N = w.shape[0]
     kb = (K + 127) // 128
-    ap, as_ = _matrix(a, M, K, _E4M3, "a")
-    wp, ws = _matrix(w, N, K, _E4M3, "w")
+    ap, _, as_ = _matrix(a, M, K, _E4M3, "a")
+    wp, _, ws = _matrix(w, N, K, _E4M3, "w")
     sap, sar, sab = _scales(a_scales, M, kb, "a_scales")
     swp, swr, swb = _scales(w_scales, (N + 127) // 128, kb, "w_scales")
-    op, os_ = _matrix(out, M, N, (torch.float32, torch.bfloat16), "out")
-    _call("srm_k_gemm_fp8", (a, a_scales, w, w_scales, out, bias, status), M, N, K, ap, as_, sap, sar, sab, wp, ws, swp, swr, swb,
-          _vector(bias, N, torch.float32, "bias"), int(accumulate), op, _CODES[out.dtype], os_, _status_word(status))
+    op, oc, os_ = _matrix(out, M, N, _OUT_CODES, "out")
+    bp, st = _vector(bias, N, _F32, "bias"), _status_word(status)
+    _run("srm_k_gemm_fp8", _device_of(a, a_scales, w, w_scales, out, bias, status), M, N, K, ap, as_, sap, sar, sab, wp, ws, swp, swr,
+         swb, bp, 1 if accumulate else 0, op, oc, os_, st)
 
 
 def k_sample(logits, u, tok, temperature=None, top_k=None, top_p=None, min_p=None, status=None):
     """A token per row of logits [R, V] (fp32, bf16 or fp16, rows may be strided) from the random numbers u [R] in [0, 1), with
     each row's own temperature, top_p, min_p (fp32 [R]) and top_k (int32 [R]), each of them optional (srm_k_sample says what they
     keep and in which order). Writes tok int32 [R]."""
-    _need(logits.dim() == 2, "logits: must be [R, V]")
     R, V = logits.shape
-    lp, ls = _matrix(logits, R, V, _CODES, "logits")
-    up, tp = _vector(u, R, torch.float32, "u"), _vector(tok, R, torch.int32, "tok")
-    _need(up is not None and tp is not None, "u, tok: missing")
-    _call("srm_k_sample", (logits, u, tok, temperature, top_k, top_p, min_p, status), R, V, lp, _CODES[logits.dtype], ls, up,
-          _vector(temperature, R, torch.float32, "temperature"), _vector(top_k, R, torch.int32, "top_k"),
-          _vector(top_p, R, torch.float32, "top_p"), _vector(min_p, R, torch.float32, "min_p"), tp, _status_word(status))
+    lp, lc, ls = _matrix(logits, R, V, _CODES, "logits")
+    if u is None or tok is None:
+        raise ValueError("u, tok: missing")
+    up, tp = _vector(u, R, _F32, "u"), _vector(tok, R, _INT32, "tok")
+    Tp, kp = _vector(temperature, R, _F32, "temperature"), _vector(top_k, R, _INT32, "top_k")
+    pp, mp, st = _vector(top_p, R, _F32, "top_p"), _vector(min_p, R, _F32, "min_p"), _status_word(status)
+    _run("srm_k_sample", _device_of(logits, u, tok, temperature, top_k, top_p, min_p, status), R, V, lp, lc, ls, up, Tp, kp, pp, mp, tp, st)
 
 
 class SRMState:

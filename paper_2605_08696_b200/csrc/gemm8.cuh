@@ -152,6 +152,7 @@ __global__ void __launch_bounds__(Few<NT>::kThreads) gemm8_few_kernel(const __gr
         uint32_t r[16];
         tm_load16(t + c, r);
         tm_load_wait();
+        keep_order(r);
         if (c + 16 == F::kCols) {
           fence_before();
           __syncwarp();
@@ -217,81 +218,79 @@ __global__ void __launch_bounds__(Few<NT>::kThreads) gemm8_few_kernel(const __gr
 }
 
 // ---- many rows -----------------------------------------------------------------------------------------------
-// A CTA pair owns a 256 x 256 tile (256 rows of A over both CTAs' accumulator lanes, 256 weight rows as two halves of 128
-// columns, each half under one scale per block); persistent, tiles taken round-robin, rows fastest. Per block of K each half is
-// four MMAs (256 x 128 x 32) into one of four accumulators of 128 columns: the warps have the time of three halves to fetch one.
-// Sixteen adding warps per CTA: 32 lanes x 64 columns each, in registers until the tile's last block.
+// A CTA pair owns a 256 x 256 tile (256 rows of A over both CTAs' accumulator lanes, 256 weight rows); persistent, tiles taken
+// round-robin, rows fastest. A block of K is four MMAs (256 x 256 x 32) into one of two accumulators, which the eight adding
+// warps of each CTA (32 lanes x 128 columns each, one weight scale) fetch while the next block is multiplied. (Halves of 128
+// columns would give them the time of three halves, but an instruction of 128 columns asks shared memory for 128 bytes a clock,
+// its limit, and took 1.27 of its share of the time.) The adding warps hold 128 sums a thread and fetch 32 columns ahead of the
+// ones they add: they take the registers that the warpgroup of the loads and the MMAs gives up. A warp of its own keeps the
+// scales of the next blocks coming into shared memory (fetched by the adding warps one block ahead they cost 330 of 1220 clocks a
+// block). What bounds it now is the adding: 256 of a block's 512 clocks are the fused multiply-adds alone.
 struct Many {
-  static constexpr int kStages = 5;
-  static constexpr int kABytes = 128 * kBK, kWBytes = 128 * kBK, kHalfBytes = 64 * kBK;      // per CTA and block
+  static constexpr int kStages = 4;
+  static constexpr int kSlots = 8;                                      // blocks whose scales are there: the stages, two accumulators, one
+  static constexpr int kABytes = 128 * kBK, kWBytes = 128 * kBK;       // per CTA and block
   static constexpr int kStage = kABytes + kWBytes;
-  static constexpr int kAddWarps = 16;
-  static constexpr int kCols = 64;
-  static constexpr int kThreads = 64 + 32 * kAddWarps;
-  static constexpr int kBox = 32 * 128;                                 // staged output of a warp: 32 rows x 128 bytes
-  static constexpr int kBytes = kStages * kStage + kAddWarps * kBox + 256 + 1024;
+  static constexpr int kAddWarps = 8;
+  static constexpr int kCols = 128;
+  static constexpr int kThreads = 128 + 32 * kAddWarps;                 // 168 registers a thread at launch
+  static constexpr int kRegsFew = 40, kRegsAdd = 232;                   // 4 x 40 + 8 x 232 = 12 x 168 (warps)
+  static constexpr int kBox = 32 * 128;                                 // staged output: 32 rows x 128 bytes, two per warp
+  static constexpr int kScales = kSlots * 130 * 4;                      // per slot: 128 rows, 2 groups of 128 columns
+  static constexpr int kBytes = kStages * kStage + kAddWarps * 2 * kBox + kScales + 256 + 1024;
 };
 
-// 32 rows x 128 bytes of finished output (v: the lane's row) from row `row0`, column `col0` on: through the warp's staging box,
-// whose 16-byte pieces are swizzled as the output's tensor map has them, to the TMA unit; or, where the rows' pitch is no
-// multiple of 16 bytes (no tensor map), row by row with plain stores.
-template <typename OT>
-__device__ __forceinline__ void put_box(const Args& g, const CUtensorMap* tmD, bool mapped, uint8_t* box, int lane, int64_t row0, int64_t col0,
-                                        const uint32_t (&v)[32]) {
-  if (mapped) {
-    if (one_lane()) stores_wait_read();                                // the box before this one has been read
-  }
-  __syncwarp();
+// A warp's staging box: 32 rows x 128 bytes of finished output (v: the lane's row), the 16-byte pieces of a row swizzled as the
+// output's tensor map has them (which also spreads eight lanes over all banks).
+__device__ __forceinline__ void fill_box(uint8_t* box, int lane, const uint32_t (&v)[32]) {
 #pragma unroll
   for (int q = 0; q < 8; ++q)
     *reinterpret_cast<uint4*>(box + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-  if (mapped) {
-    fence_async();
-    __syncwarp();
-    if (one_lane()) {
-      if (sizeof(OT) == 4 && g.accumulate) tile_add(tmD, smem_addr(box), (int)col0, (int)row0);
-      else if (sizeof(OT) == 4) tile_store_streaming(tmD, smem_addr(box), (int)col0, (int)row0);
-      else tile_store(tmD, smem_addr(box), (int)col0, (int)row0);
-      stores_commit();
-    }
-  } else {
-    __syncwarp();
-    constexpr int kWords = 32 / (int)sizeof(OT) * 4;                    // elements of a box row
-    const int rows = (int)min((int64_t)32, g.M - row0);
-    for (int r = 0; r < rows; ++r) {
-      OT* o = static_cast<OT*>(g.out) + (row0 + r) * g.out_stride + col0;
+}
+
+// A filled box to rows row0 .., columns col0 .. with plain stores, row by row: outputs whose rows' pitch is no multiple of 16 bytes
+// (they have no tensor map).
+template <typename OT>
+__device__ __forceinline__ void write_box(const Args& g, const uint8_t* box, int lane, int64_t row0, int64_t col0) {
+  constexpr int kPer = 128 / (int)sizeof(OT);
+  const int rows = (int)min((int64_t)32, g.M - row0);
+  for (int r = 0; r < rows; ++r) {
+    OT* o = static_cast<OT*>(g.out) + (row0 + r) * g.out_stride + col0;
 #pragma unroll
-      for (int e = 0; e < kWords; e += 32) {
-        const int c = e + lane, byte = c * (int)sizeof(OT);
-        const OT x = *reinterpret_cast<const OT*>(box + r * 128 + ((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15)));
-        if (col0 + c < g.N) o[c] = g.accumulate ? from_float<OT>(to_float(x) + to_float(o[c])) : x;
-      }
+    for (int e = 0; e < kPer; e += 32) {
+      const int c = e + lane, byte = c * (int)sizeof(OT);
+      const OT x = *reinterpret_cast<const OT*>(box + r * 128 + ((((byte >> 4) ^ (r & 7)) << 4) | (byte & 15)));
+      if (col0 + c < g.N) o[c] = g.accumulate ? from_float<OT>(to_float(x) + to_float(o[c])) : x;
     }
-    __syncwarp();
   }
 }
 
-template <typename OT>
+// MAPPED: the output has a tensor map; BIAS: there is one. (Each its own kernel: with both in one, the code of a tile's output,
+// unrolled over 128 columns, missed the instruction cache every time and cost as much as six blocks of K.)
+template <typename OT, bool MAPPED, bool BIAS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Many::kThreads, 1)
 gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmD,
-                  const int mapped, const Args g) {
+                  const Args g) {
   using F = Many;
   pdl_trigger();
   extern __shared__ uint8_t raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   uint8_t* boxes = smem + F::kStages * F::kStage;
-  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + F::kAddWarps * F::kBox);      // leader's: both CTAs' copies of a stage
+  float* scales = reinterpret_cast<float*>(boxes + F::kAddWarps * 2 * F::kBox);
+  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + F::kAddWarps * 2 * F::kBox + F::kScales);  // leader's: both CTAs' copies of a stage
   uint64_t* empty = full + F::kStages;                                  // per CTA: the stage may be filled again
-  uint64_t* tfull = empty + F::kStages;                                 // per CTA [4]: a half's product is there
-  uint64_t* tempty = tfull + 4;                                         // leader's [4]: both CTAs' warps have fetched it
-  uint32_t* slot = reinterpret_cast<uint32_t*>(tempty + 4);
+  uint64_t* tfull = empty + F::kStages;                                 // per CTA [2]: a block's product is there
+  uint64_t* tempty = tfull + 2;                                         // leader's [2]: both CTAs' warps have fetched it
+  uint64_t* sfull = tempty + 2;                                         // per CTA [kSlots]: a block's scales are there
+  uint32_t* slot = reinterpret_cast<uint32_t*>(sfull + F::kSlots);
 
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cta_rank();
-  const int64_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  const uint32_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
   if (threadIdx.x == 0) {
     for (int s = 0; s < F::kStages; ++s) { bar_init(&full[s], 2); bar_init(&empty[s], 1); }
-    for (int a = 0; a < 4; ++a) { bar_init(&tfull[a], 1); bar_init(&tempty[a], F::kAddWarps); }
+    for (int a = 0; a < 2; ++a) { bar_init(&tfull[a], 1); bar_init(&tempty[a], 2 * F::kAddWarps); }
+    for (int a = 0; a < F::kSlots; ++a) bar_init(&sfull[a], 32);
     bar_init_fence();
   }
   if (warp == 1) tm_alloc<2>(slot, 512);
@@ -301,8 +300,9 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   const uint32_t tm = *slot;
   pdl_wait();
 
-  const int64_t m_tiles = (g.M + 255) / 256, tiles = m_tiles * ((g.N + 255) / 256);
+  const uint32_t m_tiles = (uint32_t)((g.M + 255) / 256), tiles = m_tiles * (uint32_t)((g.N + 255) / 256);      // (fits: checked)
   const int kbs = (int)((g.K + kBK - 1) / kBK);
+  if (warp < 4) give_registers<F::kRegsFew>();
   if (warp == 0) {
     if (one_lane()) {
       map_prefetch(&tmA);
@@ -310,15 +310,14 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int64_t q = first; ok && q < tiles; q += step) {
-        const int m0 = (int)(q % m_tiles) * 256 + (int)rank * 128, n0 = (int)(q / m_tiles) * 256 + (int)rank * 64;
+      for (uint32_t q = first; ok && q < tiles; q += step) {
+        const int m0 = (int)(q % m_tiles * 256 + rank * 128), n0 = (int)(q / m_tiles * 256 + rank * 128);
         for (int kb = 0; kb < kbs; ++kb) {
           if (!bar_wait(&empty[stage], phase ^ 1u, g.status)) { ok = false; break; }
           const uint32_t bar = peer_addr(smem_addr(&full[stage]), 0), dst = smem_addr(smem + stage * F::kStage);
           bar_expect(bar, F::kStage);
           tile_load<2>(dst, &tmA, bar, kb * kBK, m0);
           tile_load<2>(dst + F::kABytes, &tmW, bar, kb * kBK, n0);
-          tile_load<2>(dst + F::kABytes + F::kHalfBytes, &tmW, bar, kb * kBK, n0 + 128);
           if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -329,97 +328,144 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       int stage = 0;
       uint32_t phase = 0, it = 0;
       bool ok = true;
-      for (int64_t q = first; ok && q < tiles; q += step) {
-        for (int kb = 0; ok && kb < kbs; ++kb, ++it) {
-          if (!bar_wait(&full[stage], phase, g.status)) { ok = false; break; }
+      for (uint32_t q = first; ok && q < tiles; q += step) {
+        for (int kb = 0; kb < kbs; ++kb, ++it) {
+          const int buf = (int)(it & 1u);
+          if (!bar_wait(&full[stage], phase, g.status) || !bar_wait(&tempty[buf], ((it >> 1) & 1u) ^ 1u, g.status)) { ok = false; break; }
+          fence_after();
           const uint32_t src = smem_addr(smem + stage * F::kStage);
-          const uint64_t da = tile_desc(src);
+          const uint64_t da = tile_desc(src), dw = tile_desc(src + F::kABytes);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int buf = (int)(it & 1u) * 2 + h;
-            if (!bar_wait(&tempty[buf], ((it >> 1) & 1u) ^ 1u, g.status)) { ok = false; break; }
-            fence_after();
-            const uint64_t dw = tile_desc(src + F::kABytes + h * F::kHalfBytes);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mma8<2>(tm + buf * 128, da + 2 * k, dw + 2 * k, mma_desc(256, 128), k != 0);
-            if (h == 1) mma_commit<2>(&empty[stage]);
-            mma_commit<2>(&tfull[buf]);
-          }
+          for (int k = 0; k < 4; ++k) mma8<2>(tm + buf * 256, da + 2 * k, dw + 2 * k, mma_desc(256, 256), k != 0);
+          mma_commit<2>(&tfull[buf]);
+          mma_commit<2>(&empty[stage]);
           if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
         }
       }
     }
-  } else {
-    const int quad = warp & 3, cg = (warp - 2) >> 2, h = cg >> 1;
-    uint8_t* box = boxes + (warp - 2) * F::kBox;
-    const uint32_t drained0 = peer_addr(smem_addr(&tempty[h]), 0);
+  } else if (warp == 2) {
+    // The scales of a block take the slot of the block eight before it, whose sums are done: this block's stage is free, so the
+    // MMAs are past the block four before it, and they are never more than two ahead of the sums.
+    int stage = 0;
+    uint32_t phase = 0, it = 0;
+    bool ok = true;
+    for (uint32_t q = first; ok && q < tiles; q += step) {
+      const float* sa[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sa[j] = g.sa + min((int64_t)(q % m_tiles * 256 + rank * 128 + j * 32 + lane), g.M - 1) * g.sa_row;
+      const float* sw = g.sw + (min((int64_t)(q / m_tiles) * 256 + (lane & 1) * 128, g.N - 1) >> 7) * g.sw_row;
+      for (int kb = 0; kb < kbs; ++kb, ++it) {
+        if (!bar_wait(&empty[stage], phase ^ 1u, g.status)) { ok = false; break; }
+        float* to = scales + (it % F::kSlots) * 130;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          copy4(smem_addr(to + j * 32 + lane), sa[j]);
+          sa[j] += g.sa_blk;
+        }
+        if (lane < 2) copy4(smem_addr(to + 128 + lane), sw);
+        sw += g.sw_blk;
+        copies_arrive(&sfull[it % F::kSlots]);
+        if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    copies_wait();
+  } else if (warp >= 4) {
+    take_registers<F::kRegsAdd>();
+    const int quad = warp & 3, cg = (warp - 4) >> 2;
+    uint8_t* box = boxes + (warp - 4) * 2 * F::kBox;
+    const uint32_t drained = peer_addr(smem_addr(&tempty[0]), 0);
+    const uint32_t lanes = tm + ((uint32_t)(quad * 32) << 16) + cg * F::kCols;
     uint32_t it = 0;
     bool ok = true;
-    if (mapped && lane == 0) map_prefetch(&tmD);
-    for (int64_t q = first; ok && q < tiles; q += step) {
-      const int64_t row0 = (q % m_tiles) * 256 + rank * 128 + quad * 32, nh = (q / m_tiles) * 256 + h * 128;
-      const int64_t col0 = nh + (cg & 1) * 64;
-      const float* sa = g.sa + min(row0 + lane, g.M - 1) * g.sa_row;
-      const float* sw = g.sw + (min(nh, g.N - 1) >> 7) * g.sw_row;
+    if (MAPPED && lane == 0) map_prefetch(&tmD);
+    for (uint32_t q = first; ok && q < tiles; q += step) {
+      const int64_t row0 = q % m_tiles * 256 + rank * 128 + quad * 32, col0 = (int64_t)(q / m_tiles) * 256 + cg * F::kCols;
       float acc[F::kCols];
-#pragma unroll
-      for (int c = 0; c < F::kCols; ++c) acc[c] = 0.f;
-      float sa_next = *sa, sw_next = *sw;
-      for (int kb = 0; kb < kbs; ++kb, ++it) {
-        const float s = sa_next * sw_next;
-        if (kb + 1 < kbs) {
-          sa_next = sa[(kb + 1) * g.sa_blk];
-          sw_next = sw[(kb + 1) * g.sw_blk];
-        }
-        const int buf = (int)(it & 1u) * 2 + h;
-        if (!bar_wait(&tfull[buf], (it >> 1) & 1u, g.status)) { ok = false; break; }
+      // one block: its scales, its product; the first one sets the sums
+      auto block = [&](auto set) {
+        const uint32_t buf = it & 1u, at = it % F::kSlots;
+        if (!bar_wait(&sfull[at], (it / F::kSlots) & 1u, g.status)) return false;
+        const float s = scales[at * 130 + quad * 32 + lane] * scales[at * 130 + 128 + cg];
+        if (!bar_wait(&tfull[buf], (it >> 1) & 1u, g.status)) return false;
         fence_after();
-        const uint32_t t = tm + ((uint32_t)(quad * 32) << 16) + buf * 128 + (cg & 1) * 64;
-        uint32_t ra[16], rb[16];
-        tm_load16(t, ra);
+        const uint32_t t = lanes + buf * 256;
+        uint32_t ra[32], rb[32];
+        tm_load32(t, ra);
         tm_load_wait();
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          uint32_t (&cur)[16] = (c & 1) ? rb : ra;
-          uint32_t (&nxt)[16] = (c & 1) ? ra : rb;
-          if (c < 3) tm_load16(t + 16 * (c + 1), nxt);
+          uint32_t (&cur)[32] = (c & 1) ? rb : ra;
+          uint32_t (&nxt)[32] = (c & 1) ? ra : rb;
+          keep_order(cur);
+          if (c < 3) tm_load32(t + 32 * (c + 1), nxt);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) acc[16 * c + j] = fmaf(s, __uint_as_float(cur[j]), acc[16 * c + j]);
+          for (int j = 0; j < 32; ++j) {
+            if (set) acc[32 * c + j] = s * __uint_as_float(cur[j]);
+            else acc[32 * c + j] = fmaf(s, __uint_as_float(cur[j]), acc[32 * c + j]);
+          }
           if (c < 3) tm_load_wait();
           if (c == 2) {                                                 // everything has left tensor memory
             fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(drained0 + (uint32_t)(it & 1u) * 16u);
+            if (lane == 0) bar_arrive(drained + buf * 8u);
           }
         }
-      }
+        ++it;
+        return true;
+      };
+      ok = block(Yes());
+      for (int kb = 1; ok && kb < kbs; ++kb) ok = block(No());
       if (!ok) break;
       if (row0 < g.M && col0 < g.N) {
-        if (g.bias != nullptr) {
+        constexpr int kPer = 128 / (int)sizeof(OT);                     // columns of a box
 #pragma unroll
-          for (int c = 0; c < F::kCols; ++c) acc[c] += col0 + c < g.N ? __ldg(g.bias + col0 + c) : 0.f;
-        }
-        uint32_t v[32];
-        if (sizeof(OT) == 4) {
+        for (int c0 = 0; c0 < F::kCols; c0 += 2 * kPer) {
+          if (MAPPED && one_lane()) stores_wait_read();                 // the boxes have been read
+          __syncwarp();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(acc[j]);
-          put_box<OT>(g, &tmD, mapped, box, lane, row0, col0, v);
-          if (col0 + 32 < g.N) {
+          for (int c = c0; c < c0 + 2 * kPer; c += kPer) {
+            uint32_t v[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(acc[32 + j]);
-            put_box<OT>(g, &tmD, mapped, box, lane, row0, col0 + 32, v);
+            for (int j = 0; j < kPer; j += 2) {
+              float x = acc[c + j], y = acc[c + j + 1];
+              if (BIAS) {
+                x += col0 + c + j < g.N ? __ldg(g.bias + col0 + c + j) : 0.f;
+                y += col0 + c + j + 1 < g.N ? __ldg(g.bias + col0 + c + j + 1) : 0.f;
+              }
+              if (sizeof(OT) == 4) {
+                v[j % 32] = __float_as_uint(x);
+                v[j % 32 + 1] = __float_as_uint(y);
+              } else {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+                v[j / 2 % 32] = *reinterpret_cast<const uint32_t*>(&b);
+              }
+            }
+            fill_box(box + (c / kPer & 1) * F::kBox, lane, v);
           }
-        } else {
+          if (MAPPED) fence_async();
+          __syncwarp();
+          if (MAPPED) {
+            if (one_lane()) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(acc[2 * j], acc[2 * j + 1]);
-            v[j] = *reinterpret_cast<const uint32_t*>(&b);
+              for (int b = 0; b < 2; ++b) {
+                const int64_t col = col0 + c0 + b * kPer;
+                const uint32_t src = smem_addr(box + b * F::kBox);
+                if (col < g.N) {
+                  if (sizeof(OT) == 4 && g.accumulate) tile_add(&tmD, src, (int)col, (int)row0);
+                  else if (sizeof(OT) == 4) tile_store_streaming(&tmD, src, (int)col, (int)row0);
+                  else tile_store(&tmD, src, (int)col, (int)row0);
+                }
+              }
+              stores_commit();
+            }
+          } else {
+            write_box<OT>(g, box, lane, row0, col0 + c0);
+            write_box<OT>(g, box + F::kBox, lane, row0, col0 + c0 + kPer);
           }
-          put_box<OT>(g, &tmD, mapped, box, lane, row0, col0, v);
         }
       }
     }
-    if (mapped && one_lane()) stores_wait();                            // the boxes are out before shared memory goes away
+    if (MAPPED && one_lane()) stores_wait();                            // the boxes are out before shared memory goes away
   }
   fence_before();
   sync_cluster();                                                       // the leader's MMAs use the peer's memory until here

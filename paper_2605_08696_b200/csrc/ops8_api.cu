@@ -26,8 +26,10 @@ int rows_ok(const void* p, int64_t rows, int64_t cols, int64_t stride, int64_t e
   return SRM_OK;
 }
 int floats_ok(const void* p) { return p == nullptr ? SRM_ERR_INVALID_ARG : !aligned(p, 4) ? SRM_ERR_ALIGNMENT : SRM_OK; }
-// Scales of a matrix: any positive strides.
-int scales_ok(const float* p, int64_t row, int64_t blk) { return row < 1 || blk < 1 ? SRM_ERR_INVALID_ARG : floats_ok(p); }
+// Scales of a matrix, rows x blks of them: written ones each in a place of their own, read ones with any stride from 0.
+int scales_ok(const float* p, int64_t rows, int64_t blks, int64_t row, int64_t blk, int64_t least) {
+  return (rows > 1 && row < least) || (blks > 1 && blk < least) ? SRM_ERR_INVALID_ARG : floats_ok(p);
+}
 
 constexpr int64_t kMaxGrid = 0x7fffffff;
 
@@ -89,21 +91,22 @@ int launch_few(const g8::Args& g, const uint8_t* A, int64_t a_stride, const uint
 
 template <typename OT>
 int launch_many(const g8::Args& g, const uint8_t* A, int64_t a_stride, const uint8_t* W, int64_t w_stride, int sms, cudaStream_t st) {
-  const auto kernel = g8::gemm8_many_kernel<OT>;
+  const int elem = (int)sizeof(OT);
+  const int64_t pitch = map_stride(g.M, g.N, g.out_stride, elem);
+  const bool mapped = aligned(g.out, 16) && pitch * elem % 16 == 0;
+  const auto kernel = mapped ? (g.bias != nullptr ? g8::gemm8_many_kernel<OT, true, true> : g8::gemm8_many_kernel<OT, true, false>)
+                             : (g.bias != nullptr ? g8::gemm8_many_kernel<OT, false, true> : g8::gemm8_many_kernel<OT, false, false>);
   int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), g8::Many::kBytes);
   if (rc != SRM_OK) return rc;
   CUtensorMap ta, tw, td;
   if ((rc = byte_map(&ta, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, g.M, g.K, map_stride(g.M, g.K, a_stride, 1), 128)) != SRM_OK) return rc;
-  if ((rc = byte_map(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, W, g.N, g.K, map_stride(g.N, g.K, w_stride, 1), 64)) != SRM_OK) return rc;
-  const int elem = (int)sizeof(OT);
-  const int64_t pitch = map_stride(g.M, g.N, g.out_stride, elem);
-  const int mapped = aligned(g.out, 16) && pitch * elem % 16 == 0;
+  if ((rc = byte_map(&tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, W, g.N, g.K, map_stride(g.N, g.K, w_stride, 1), 128)) != SRM_OK) return rc;
   td = ta;
   if (mapped && (rc = byte_map(&td, elem == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, elem, g.out, g.M, g.N, pitch, 32)) != SRM_OK)
     return rc;
   const int64_t tiles = (g.M + 255) / 256 * ((g.N + 255) / 256), pairs = sms / 2;
   ++g_kernel_launches;
-  SRM_CUDA(launch_kernel(kernel, dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(g8::Many::kThreads), g8::Many::kBytes, st, ta, tw, td, mapped, g));
+  SRM_CUDA(launch_kernel(kernel, dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(g8::Many::kThreads), g8::Many::kBytes, st, ta, tw, td, g));
   return SRM_OK;
 }
 
@@ -113,6 +116,7 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   const int rc = device_sm_count(&sms);
   if (rc != SRM_OK) return rc;
   const int64_t n_tiles = (g.N + 127) / 128, kb = (g.K + 127) / 128;
+  if ((g.M + 255) / 256 * ((g.N + 255) / 256) > 0x3fffffff) return SRM_ERR_UNSUPPORTED;
   if (g.M > 256 && g.N > 128) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
   const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
   const int64_t m_tiles = (g.M + nt - 1) / nt;
@@ -143,7 +147,7 @@ int srm_k_rms_norm_fp8(int64_t R, int32_t d, const void* d_x, int32_t x_dtype, i
   if (d_sum != nullptr && (rc = rows_ok(d_sum, R, d, sum_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
   if ((rc = rows_ok(d_q, R, d, q_stride, 1)) != SRM_OK) return rc;
   if ((rc = rows_ok(d_g, 1, d, d, 4)) != SRM_OK) return rc;
-  if ((rc = scales_ok(d_scale, scale_row, scale_blk)) != SRM_OK) return rc;
+  if ((rc = scales_ok(d_scale, R, (d + 127) / 128, scale_row, scale_blk, 1)) != SRM_OK) return rc;
   const q8::NormArgs p{R, d, d_x, x_stride, d_delta, delta_stride, d_g, eps, d_sum, sum_stride, d_q, q_stride, d_scale, scale_row, scale_blk};
   return with_type(x_dtype, [&](auto x) {
     return with_type(d_delta != nullptr ? delta_dtype : SRM_DTYPE_FP32,
@@ -162,7 +166,7 @@ int srm_k_quant_fp8(int64_t R, int64_t K, const void* d_x, int32_t x_dtype, int6
   int rc;
   if ((rc = rows_ok(d_x, R, K, x_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
   if ((rc = rows_ok(d_q, R, K, q_stride, 1)) != SRM_OK) return rc;
-  if ((rc = scales_ok(d_scale, scale_row, scale_blk)) != SRM_OK) return rc;
+  if ((rc = scales_ok(d_scale, (R + block_rows - 1) / block_rows, kb, scale_row, scale_blk, 1)) != SRM_OK) return rc;
   const q8::QuantArgs p{R, K, d_x, x_stride, d_q, q_stride, d_scale, scale_row, scale_blk};
   return with_type(x_dtype, [&](auto x) -> int {
     using XT = decltype(x);
@@ -184,7 +188,8 @@ int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t 
   int rc;
   if ((rc = rows_ok(d_A, M, K, a_stride, 1)) != SRM_OK) return rc;
   if ((rc = rows_ok(d_W, N, K, w_stride, 1)) != SRM_OK) return rc;
-  if ((rc = scales_ok(d_sa, sa_row, sa_blk)) != SRM_OK || (rc = scales_ok(d_sw, sw_row, sw_blk)) != SRM_OK) return rc;
+  const int64_t kb = (K + 127) / 128;
+  if ((rc = scales_ok(d_sa, M, kb, sa_row, sa_blk, 0)) != SRM_OK || (rc = scales_ok(d_sw, (N + 127) / 128, kb, sw_row, sw_blk, 0)) != SRM_OK) return rc;
   if (d_bias != nullptr && (rc = floats_ok(d_bias)) != SRM_OK) return rc;
   if (d_out == nullptr || (M > 1 && out_stride < N)) return SRM_ERR_INVALID_ARG;
   if (!aligned(d_out, (size_t)dtype_bytes(out_dtype))) return SRM_ERR_ALIGNMENT;

@@ -26,10 +26,22 @@ __device__ __forceinline__ uint32_t abs_max4(float4 v) {
   return max(max(abs_bits(v.x), abs_bits(v.y)), max(abs_bits(v.z), abs_bits(v.w)));
 }
 
-// four values times `inv`, as e4m3 bytes (the conversion of a NaN is the NaN code)
-__device__ __forceinline__ uint32_t pack4(float4 v, float inv) {
-  const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v.x * inv, v.y * inv), __NV_SATFINITE, __NV_E4M3);
-  const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v.z * inv, v.w * inv), __NV_SATFINITE, __NV_E4M3);
+// A block's divisor: x / s as x * (1 / s) and one correction by the remainder, which gives the quotient's own rounding. (The
+// product alone is off by up to two roundings, and bf16 values over the scale of a bf16 maximum lie halfway between two codes
+// often enough for that to show.) An infinite scale has no remainder.
+struct Divisor {
+  float inv, s;
+  __device__ explicit Divisor(float scale) : inv(1.0f / scale), s(scale < INFINITY ? scale : 0.0f) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    const float q = x * inv;
+    return fmaf(fmaf(-q, s, x), inv, q);
+  }
+};
+
+// four values over their block's scale, as e4m3 bytes (the conversion of a NaN is the NaN code)
+__device__ __forceinline__ uint32_t pack4(float4 v, const Divisor& d) {
+  const __nv_fp8x2_storage_t lo = __nv_cvt_float2_to_fp8x2(make_float2(d(v.x), d(v.y)), __NV_SATFINITE, __NV_E4M3);
+  const __nv_fp8x2_storage_t hi = __nv_cvt_float2_to_fp8x2(make_float2(d(v.z), d(v.w)), __NV_SATFINITE, __NV_E4M3);
   return (uint32_t)lo | ((uint32_t)hi << 16);
 }
 
@@ -116,7 +128,7 @@ __global__ void rms_norm_fp8_kernel(const NormArgs p) {
     }
     const float s = block_scale(__reduce_max_sync(0xffffffffu, abs_max4(y)));
     if (i < n4) {
-      *reinterpret_cast<uint32_t*>(p.q + row * p.q_stride + 4 * i) = pack4(y, 1.0f / s);
+      *reinterpret_cast<uint32_t*>(p.q + row * p.q_stride + 4 * i) = pack4(y, Divisor(s));
       if (lane == 0) p.scale[row * p.scale_row + (i >> 5) * p.scale_blk] = s;
     }
   }
@@ -146,7 +158,7 @@ __global__ void __launch_bounds__(kQuantThreads) quant_rows_kernel(const QuantAr
   const bool in = c < p.K;
   const float4 v = in ? ld4(static_cast<const XT*>(p.x) + row * p.x_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
   const float s = block_scale(__reduce_max_sync(0xffffffffu, abs_max4(v)));
-  if (in) *reinterpret_cast<uint32_t*>(p.q + row * p.q_stride + c) = pack4(v, 1.0f / s);
+  if (in) *reinterpret_cast<uint32_t*>(p.q + row * p.q_stride + c) = pack4(v, Divisor(s));
   if (lane == 0) p.scale[row * p.scale_row + b * p.scale_blk] = s;
 }
 
@@ -174,11 +186,12 @@ __global__ void __launch_bounds__(kQuantThreads) quant_tiles_kernel(const QuantA
   if (lane == 0) part[warp] = m;
   __syncthreads();
   m = __reduce_max_sync(0xffffffffu, part[lane & (kQuantThreads / 32 - 1)]);
-  const float s = block_scale(m), inv = 1.0f / s;
+  const float s = block_scale(m);
+  const Divisor by(s);
 #pragma unroll
   for (int j = 0; j < kRowsPerWarp; ++j) {
     const int64_t r = rb * 128 + j * (kQuantThreads / 32) + warp;
-    if (in && r < p.R) *reinterpret_cast<uint32_t*>(p.q + r * p.q_stride + c) = pack4(v[j], inv);
+    if (in && r < p.R) *reinterpret_cast<uint32_t*>(p.q + r * p.q_stride + c) = pack4(v[j], by);
   }
   if (threadIdx.x == 0) p.scale[rb * p.scale_row + b * p.scale_blk] = s;
 }

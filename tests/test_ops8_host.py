@@ -44,18 +44,18 @@ def _sample(**kw):
     (_norm, dict(d=120), UNSUPPORTED), (_norm, dict(d=16400), UNSUPPORTED), (_norm, dict(x=None), INVALID), (_norm, dict(q=None), INVALID),
     (_norm, dict(g=None), INVALID), (_norm, dict(s=None), INVALID), (_norm, dict(xs=127), INVALID), (_norm, dict(x=A + 4), ALIGNMENT),
     (_norm, dict(xs=130), ALIGNMENT), (_norm, dict(qs=136), ALIGNMENT), (_norm, dict(q=A + 8), ALIGNMENT), (_norm, dict(g=A + 4), ALIGNMENT),
-    (_norm, dict(s=A + 2), ALIGNMENT), (_norm, dict(sr=0), INVALID), (_norm, dict(sb=-1), INVALID), (_norm, dict(dl=A + 2, ds=128), ALIGNMENT),
+    (_norm, dict(s=A + 2), ALIGNMENT), (_norm, dict(sr=0), INVALID), (_norm, dict(d=256, xs=256, qs=256, sb=0), INVALID), (_norm, dict(dl=A + 2, ds=128), ALIGNMENT),
     (_norm, dict(dl=A, ds=128, h=A, hs=64), INVALID), (_norm, dict(R=0, x=None), OK),
     (_quant, dict(R=-2), INVALID), (_quant, dict(K=0), INVALID), (_quant, dict(K=100), UNSUPPORTED), (_quant, dict(br=2), INVALID),
     (_quant, dict(br=0), INVALID), (_quant, dict(xt=-1), INVALID), (_quant, dict(x=None), INVALID), (_quant, dict(x=A + 2), ALIGNMENT),
     (_quant, dict(xs=132), ALIGNMENT), (_quant, dict(qs=132), ALIGNMENT), (_quant, dict(qs=112), INVALID), (_quant, dict(s=None), INVALID),
-    (_quant, dict(sb=0), INVALID), (_quant, dict(R=1 << 40), UNSUPPORTED), (_quant, dict(R=0, q=None), OK),
+    (_quant, dict(K=144, xs=144, qs=144, sb=0), INVALID), (_quant, dict(R=1 << 40), UNSUPPORTED), (_quant, dict(R=0, q=None), OK),
     (_gemm, dict(M=-1), INVALID), (_gemm, dict(N=0), INVALID), (_gemm, dict(K=0), INVALID), (_gemm, dict(K=24), UNSUPPORTED),
     (_gemm, dict(ot=2), INVALID), (_gemm, dict(acc=2), INVALID), (_gemm, dict(acc=1, ot=1), UNSUPPORTED), (_gemm, dict(A=None), INVALID),
     (_gemm, dict(W=None), INVALID), (_gemm, dict(sa=None), INVALID), (_gemm, dict(sw=None), INVALID), (_gemm, dict(out=None), INVALID),
     (_gemm, dict(A=A + 1), ALIGNMENT), (_gemm, dict(W=A + 8), ALIGNMENT), (_gemm, dict(as_=136), ALIGNMENT), (_gemm, dict(ws=120), INVALID),
-    (_gemm, dict(out=A + 2), ALIGNMENT), (_gemm, dict(out=A + 1, ot=1), ALIGNMENT), (_gemm, dict(os=7), INVALID), (_gemm, dict(sar=0), INVALID),
-    (_gemm, dict(swb=0), INVALID), (_gemm, dict(bias=A + 2), ALIGNMENT), (_gemm, dict(M=0, A=None), OK),
+    (_gemm, dict(out=A + 2), ALIGNMENT), (_gemm, dict(out=A + 1, ot=1), ALIGNMENT), (_gemm, dict(os=7), INVALID), (_gemm, dict(sar=-1), INVALID),
+    (_gemm, dict(N=200, os=200, swr=-1), INVALID), (_gemm, dict(bias=A + 2), ALIGNMENT), (_gemm, dict(M=0, A=None), OK),
     (_sample, dict(R=-1), INVALID), (_sample, dict(V=0), INVALID), (_sample, dict(V=262145, ls=262145), UNSUPPORTED), (_sample, dict(lt=5), INVALID),
     (_sample, dict(l=None), INVALID), (_sample, dict(u=None), INVALID), (_sample, dict(tok=None), INVALID), (_sample, dict(ls=7), INVALID),
     (_sample, dict(l=A + 2), ALIGNMENT), (_sample, dict(l=A + 1, lt=1), ALIGNMENT), (_sample, dict(T=A + 1), ALIGNMENT),
