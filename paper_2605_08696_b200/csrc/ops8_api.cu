@@ -129,6 +129,45 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   return launch_few<128, OT>(g, A, a_stride, W, w_stride, ranks, st);
 }
 
+// A block per row, a warp per 1024 ids; a cluster of blocks per row where one block's registers do not hold it.
+template <typename T>
+int launch_sample(const smp::Args& p, cudaStream_t st) {
+  const int stretches = (p.V + smp::kWarpIds - 1) / smp::kWarpIds;
+  ++g_kernel_launches;
+  if (stretches <= smp::kMaxWarps) {
+    SRM_CUDA(launch_kernel(smp::sample_kernel<T, false>, dim3((unsigned)p.R), dim3(32 * stretches), 0, st, p, stretches * smp::kWarpIds));
+    return SRM_OK;
+  }
+  int ranks = 2;
+  while (ranks * smp::kMaxWarps < stretches) ranks *= 2;
+  const int warps = (stretches + ranks - 1) / ranks;
+  for (int64_t r0 = 0; r0 < p.R; r0 += 65535) {                  // (rows are the grid's second dimension)
+    smp::Args q = p;
+    q.R = p.R - r0 < 65535 ? p.R - r0 : 65535;
+    q.logits = static_cast<const T*>(p.logits) + r0 * p.stride;
+    q.u = p.u + r0;
+    if (p.temperature != nullptr) q.temperature = p.temperature + r0;
+    if (p.top_k != nullptr) q.top_k = p.top_k + r0;
+    if (p.top_p != nullptr) q.top_p = p.top_p + r0;
+    if (p.min_p != nullptr) q.min_p = p.min_p + r0;
+    q.tok = p.tok + r0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ranks, (unsigned)q.R);
+    cfg.blockDim = dim3(32 * warps);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ranks; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (r0 > 0) ++g_kernel_launches;
+    SRM_CUDA(cudaLaunchKernelEx(&cfg, smp::sample_kernel<T, true>, q, warps * smp::kWarpIds));
+  }
+  return SRM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -210,12 +249,7 @@ int srm_k_sample(int64_t R, int32_t V, const void* d_logits, int32_t logits_dtyp
       !aligned(d_top_p, 4) || !aligned(d_min_p, 4) || !aligned(d_tok, 4) || !aligned(d_status, 4))
     return SRM_ERR_ALIGNMENT;
   const smp::Args p{R, V, d_logits, logits_stride, d_u, d_temperature, d_top_k, d_top_p, d_min_p, d_tok, d_status};
-  return with_type(logits_dtype, [&](auto t) -> int {
-    ++g_kernel_launches;
-    SRM_CUDA(launch_kernel(smp::sample_simple_kernel<decltype(t)>, dim3((unsigned)R), dim3(smp::kSimpleThreads), 0,
-                           static_cast<cudaStream_t>(stream), p));
-    return SRM_OK;
-  });
+  return with_type(logits_dtype, [&](auto t) { return launch_sample<decltype(t)>(p, static_cast<cudaStream_t>(stream)); });
 }
 
 }  // extern "C"
