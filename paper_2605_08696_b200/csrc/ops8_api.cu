@@ -129,42 +129,35 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   return launch_few<128, OT>(g, A, a_stride, W, w_stride, ranks, st);
 }
 
-// A block per row, a warp per 1024 ids; a cluster of blocks per row where one block's registers do not hold it.
+// Many rows: a block of up to 512 threads each, three per SM (their rows fit in L2 together). Few rows of many ids: a cluster of
+// blocks each, so that a pass is as short as for 32768 ids or fewer.
 template <typename T>
 int launch_sample(const smp::Args& p, cudaStream_t st) {
-  const int stretches = (p.V + smp::kWarpIds - 1) / smp::kWarpIds;
+  int sms = 0;
+  const int rc = device_sm_count(&sms);
+  if (rc != SRM_OK) return rc;
+  const int stretches = (p.V + smp::kStretch - 1) / smp::kStretch;
   ++g_kernel_launches;
-  if (stretches <= smp::kMaxWarps) {
-    SRM_CUDA(launch_kernel(smp::sample_kernel<T, false>, dim3((unsigned)p.R), dim3(32 * stretches), 0, st, p, stretches * smp::kWarpIds));
+  int ranks = 1;
+  while (ranks < smp::kMaxRanks && stretches > 64 * ranks && 2 * ranks * p.R <= sms) ranks *= 2;
+  if (ranks == 1) {
+    const int warps = stretches < 16 ? stretches : 16;
+    SRM_CUDA(launch_kernel(smp::sample_kernel<T, false>, dim3((unsigned)p.R), dim3(32 * warps), 0, st, p, stretches));
     return SRM_OK;
   }
-  int ranks = 2;
-  while (ranks * smp::kMaxWarps < stretches) ranks *= 2;
-  const int warps = (stretches + ranks - 1) / ranks;
-  for (int64_t r0 = 0; r0 < p.R; r0 += 65535) {                  // (rows are the grid's second dimension)
-    smp::Args q = p;
-    q.R = p.R - r0 < 65535 ? p.R - r0 : 65535;
-    q.logits = static_cast<const T*>(p.logits) + r0 * p.stride;
-    q.u = p.u + r0;
-    if (p.temperature != nullptr) q.temperature = p.temperature + r0;
-    if (p.top_k != nullptr) q.top_k = p.top_k + r0;
-    if (p.top_p != nullptr) q.top_p = p.top_p + r0;
-    if (p.min_p != nullptr) q.min_p = p.min_p + r0;
-    q.tok = p.tok + r0;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ranks, (unsigned)q.R);
-    cfg.blockDim = dim3(32 * warps);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)ranks; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    if (r0 > 0) ++g_kernel_launches;
-    SRM_CUDA(cudaLaunchKernelEx(&cfg, smp::sample_kernel<T, true>, q, warps * smp::kWarpIds));
-  }
+  const int per_rank = (stretches + ranks - 1) / ranks, warps = per_rank < smp::kMaxWarps ? per_rank : smp::kMaxWarps;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ranks, (unsigned)p.R);                  // (few rows)
+  cfg.blockDim = dim3(32 * warps);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)ranks; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  SRM_CUDA(cudaLaunchKernelEx(&cfg, smp::sample_kernel<T, true>, p, per_rank));
   return SRM_OK;
 }
 

@@ -5,12 +5,13 @@
 //   tokens with w_i >= min_p; then the lowest id whose cumulative mass, ids ascending, exceeds u times the mass kept.
 // What is kept is always a prefix of the order.
 //
-// A row is read once: its weights stay in the registers of one block (32 per thread; a cluster of blocks where the vocabulary is
-// longer than 32768) as fp32 values whose error is bounded (kSlack). Borders are searched on those: a threshold probe costs
-// three instructions per element and a reduction. The few tokens that the bounds leave undecided (at most kCap of them, or all
-// that can be kept when these are so few) go to shared memory, where they are sorted and weighed in 64 bits; sums that a decision
-// depends on more closely than the bounds allow are formed again in 64 bits from the logits, in a second read that finds them in
-// L2. So the token is the one that 64-bit arithmetic gives, and nearly all of the arithmetic is not 64-bit.
+// A block takes a row (a cluster of blocks, where there are few rows and many ids) and passes over it as often as the row needs,
+// from HBM the first time, from L2 after that; several blocks per SM overlap their passes. First pass: the maximum, and each
+// thread's own one; the k-th largest of those is a threshold that at least k tokens reach, and few more. Second pass: the tokens
+// that reach it go to shared memory, where they are sorted and weighed in 64 bits; that is all for top-k, and for a nucleus that
+// lies inside them. Otherwise the border is closed in on by thresholds, three per pass, with fp32 masses whose error is bounded
+// (kSlack), until at most kCap tokens are left undecided; those are decided in 64 bits, with 64-bit sums over the rest where the
+// bounds do not suffice. So the token is the one that 64-bit arithmetic gives, and nearly all of the arithmetic is not 64-bit.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -47,27 +48,30 @@ template <typename T> __device__ __forceinline__ float load_logit(const Args& p,
   return to_float(static_cast<const T*>(p.logits)[row * p.stride + i]);
 }
 
-constexpr int kWarpIds = 1024;                   // consecutive ids of a warp: 8 groups of 128, four per lane
+constexpr int kStretch = 512;                    // consecutive ids that a warp reads at a time: four groups of 128, four per lane
+constexpr int kMaxStretches = 512;               // 262144 ids
 constexpr int kMaxWarps = 32;
 constexpr int kCap = 1024;                       // tokens that are sorted
 constexpr int kMaxRanks = 8;
-// Bound on the relative error of an fp32 weight above kLeast and of sums of them: the difference to the maximum, the factor
-// 1 / (T ln 2) and their product are rounded once each, which moves a weight 2^x by 3 |x| 2^-24 ln 2 (|x| <= 80: 1.0e-5), ex2 by
-// 2^-22, a thread's sum of 32 and two levels of five by 42 roundings (2.5e-6).
-constexpr float kSlack = 2e-5f;
-constexpr float kLeast = 8.271806125530277e-25f; // 2^-80: all weights below it together are under 64-bit rounding (2^18 ids)
-constexpr int kProbes = 40;
+// Bound on the relative error of a sum of fp32 weights above 2^-80: the difference to the maximum, the factor 1 / (T ln 2) and
+// their product are rounded once each, which moves a weight 2^x by 3 |x| 2^-24 ln 2 (|x| <= 80: 1.0e-5), ex2 by 2^-22, and the sums
+// of at most 512 weights in a thread's run and two levels of five add 522 roundings (3.2e-5).
+constexpr float kSlack = 5e-5f;
+constexpr double kSlack64 = 1e-11;               // the same for weights and sums in 64 bits
+constexpr double kLeastLog2 = -80.0;             // all weights below 2^-80 together are under 64-bit rounding (2^18 ids)
+constexpr int kRounds = 40;                      // of a search: every other one takes two bits off the distance of lo and hi as keys
 
 // 2^y for y <= 0 in 64 bits: the power of two by the exponent field, the rest by the series of exp to the 12th power of an
-// argument of at most ln 2 / 2 (the remainder is under 2e-16).
+// argument of at most ln 2 / 2 (the remainder is under 2e-16). Rounding to the whole number by adding 1.5 2^52, whose low word then
+// holds it (the conversion instructions have an eighth of the rate).
 __device__ __forceinline__ double pow2_64(double y) {
   if (!(y > -1000.0)) return 0.0;
-  const double n = rint(y), t = (y - n) * 0.693147180559945309417;
+  const double shifted = y + 6755399441055744.0, n = shifted - 6755399441055744.0, t = (y - n) * 0.693147180559945309417;
   double s = 1.0 / 479001600;
   s = fma(s, t, 1.0 / 39916800); s = fma(s, t, 1.0 / 3628800); s = fma(s, t, 1.0 / 362880); s = fma(s, t, 1.0 / 40320);
   s = fma(s, t, 1.0 / 5040); s = fma(s, t, 1.0 / 720); s = fma(s, t, 1.0 / 120); s = fma(s, t, 1.0 / 24); s = fma(s, t, 1.0 / 6);
   s = fma(s, t, 0.5); s = fma(s, t, 1.0); s = fma(s, t, 1.0);
-  return __hiloint2double(__double2hiint(s) + ((int)n << 20), __double2loint(s));
+  return __hiloint2double(__double2hiint(s) + (__double2loint(shifted) << 20), __double2loint(s));
 }
 
 // Weight of a token in 64 bits; l_max itself (infinite or not) has 1. `rate`: 1 / (T ln 2).
@@ -92,25 +96,19 @@ __device__ __forceinline__ unsigned long long word_of(float l, int id) {
 }
 __device__ __forceinline__ float word_logit(unsigned long long w) { return key_logit(~(uint32_t)(w >> 32)); }
 
-// Parameters of a row, the same in every thread.
-struct RowArgs {
-  int64_t row;
-  float l_max;
-  double rate;                 // 1 / (T ln 2)
-  int top_k;                   // 1 .. V
-  double top_p, min_p;         // top_p >= 1, min_p = 0: no effect
-  double u;
-};
-
 struct Scratch {
   unsigned long long cand[kCap];
   double weight[kCap], run[kCap];      // of the sorted candidates: weights, and running sums of them
-  double warp_sum[kMaxRanks * kMaxWarps];
+  double part[kMaxStretches];          // mass kept of each stretch
+  uint32_t ties[kMaxStretches];
   double d[2][kMaxWarps], rank_d[2][kMaxRanks];
   float f[2][kMaxWarps], rank_f[2][kMaxRanks];
   uint32_t n[2][kMaxWarps], rank_n[2][kMaxRanks];
+  float f3[3][kMaxWarps], rank_f3[3][kMaxRanks];
+  uint32_t n3[3][kMaxWarps], rank_n3[3][kMaxRanks];
   uint32_t count;
   int keep, unsure, tok, last;
+  double box[2];                       // from the leading rank to the others
 };
 
 // What a block (or, with CL, a cluster) knows and does together. Reductions use two sets of places in turn, so one barrier each is
@@ -211,6 +209,21 @@ __device__ inline void sort_words(unsigned long long* w, int n, int tid, int thr
     }
 }
 
+// The same for short lists, by counting: eight lanes per word find how many are smaller. `from` and `to` are different.
+__device__ inline void sort_short(const unsigned long long* from, unsigned long long* to, int n, int tid, int threads) {
+  for (int c0 = 0; c0 < n; c0 += threads >> 3) {
+    const int c = c0 + (tid >> 3);
+    const unsigned long long mine = c < n ? from[c] : 0ull;
+    int rank = 0;
+    for (int j = tid & 7; j < n; j += 8) rank += from[j] < mine ? 1 : 0;
+    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+    rank += __shfl_xor_sync(0xffffffffu, rank, 4);
+    if (c < n && (tid & 7) == 0) to[rank] = mine;
+  }
+  __syncthreads();
+}
+
 // run[i] = d[0] + .. + d[i] for i < n: each thread a run of consecutive places, in a fixed order.
 __device__ inline void running_sums(const double* d, double* run, int n, int tid, int threads, double* part) {
   const int per = (n + threads - 1) / threads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
@@ -235,299 +248,258 @@ __device__ inline void running_sums(const double* d, double* run, int n, int tid
   __syncthreads();
 }
 
-// ---- rows whose border the search cannot close in on --------------------------------------------------------------
-// (Thousands of tokens with one and the same weight.) One block, all in 64 bits: the border key bit by bit, a pass over the row
-// each, then the ids in order.
-template <typename T>
-__device__ __noinline__ int slow_row(const Args& p, const RowArgs& a, Scratch& s) {
-  Group<false> g{s, (int)threadIdx.x, (int)threadIdx.x & 31, (int)threadIdx.x >> 5, (int)blockDim.x >> 5, 0, 1};
-  const int threads = blockDim.x;
-  double mass;
-  uint32_t count;
-  auto above = [&](uint32_t t) {
-    mass = 0.0;
-    count = 0;
-    for (int i = g.tid; i < p.V; i += threads) {
-      const float l = load_logit<T>(p, a.row, i);
-      const uint32_t k = logit_key(l);
-      if (k != 0u && k >= t) { mass += weight64(l, a.l_max, a.rate); ++count; }
-    }
-    float none = 0.f;
-    mass = g.add64(mass);
-    g.add(none, count);
-  };
-  uint32_t t = 1u, m = 0xffffffffu;                  // keys above t are kept, and at t the m lowest ids
-  above(1u);
-  double Z1 = mass;
-  if (count > (uint32_t)a.top_k) {
-    uint32_t key = 0;
-    for (int b = 31; b >= 0; --b) {
-      above(key | (1u << b));
-      if (count >= (uint32_t)a.top_k) key |= 1u << b;
-    }
-    t = key;
-    above(t + 1u);
-    m = (uint32_t)a.top_k - count;
-    Z1 = mass + (double)m * weight64(key_logit(t), a.l_max, a.rate);
-  }
-  if (a.top_p < 1.0) {
-    const double want = a.top_p * Z1;
-    uint32_t key = 0;                                // the largest key whose mass reaches `want`
-    for (int b = 31; b >= 0; --b) {
-      above(key | (1u << b));
-      if (count != 0 && (want <= 0.0 || mass >= want)) key |= 1u << b;
-    }
-    if (key >= t) {
-      above(key + 1u);
-      const double w = weight64(key_logit(key), a.l_max, a.rate);
-      const uint32_t most = key == t ? m : (uint32_t)p.V;
-      // the first c >= 1 with mass + c w >= want
-      double c = w > 0.0 ? ceil((want - mass) / w) : 1.0;
-      c = c < 1.0 ? 1.0 : c;
-      while (c > 1.0 && mass + (c - 1.0) * w >= want) c -= 1.0;
-      while (c < (double)most && mass + c * w < want) c += 1.0;
-      t = key;
-      m = c < (double)most ? (uint32_t)c : most;
-    }
-  }
-  double Z = 0.0;
-  __syncthreads();
-  if (g.tid == 0) { s.tok = 0x7fffffff; s.last = -1; }
-  for (int pass = 0; pass < 2; ++pass) {
-    const double target = a.u * Z;
-    double run = 0.0;
-    uint32_t ties = 0;
-    for (int base = 0; base < p.V; base += threads) {
-      const int i = base + g.tid;
-      uint32_t k = 0;
-      double w = 0.0;
-      if (i < p.V) {
-        const float l = load_logit<T>(p, a.row, i);
-        k = logit_key(l);
-        if (k >= t && k != 0u) w = weight64(l, a.l_max, a.rate);
-        if (!(w >= a.min_p)) { w = 0.0; k = 0; }
-      }
-      const bool tie = k != 0u && k == t;
-      const uint32_t bal = __ballot_sync(0xffffffffu, tie);
-      __syncthreads();
-      if (g.lane == 0) s.n[0][g.warp] = __popc(bal);
-      __syncthreads();
-      uint32_t before = ties;
-      for (int q = 0; q < g.warps; ++q) { if (q < g.warp) before += s.n[0][q]; ties += s.n[0][q]; }
-      before += __popc(bal & ((1u << g.lane) - 1u));
-      const bool kept = k > t || (tie && before < m);
-      double incl = kept ? w : 0.0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const double x = __shfl_up_sync(0xffffffffu, incl, o);
-        if (g.lane >= o) incl += x;
-      }
-      if (g.lane == 31) s.d[0][g.warp] = incl;
-      __syncthreads();
-      double off = run;
-      for (int q = 0; q < g.warps; ++q) { if (q < g.warp) off += s.d[0][q]; run += s.d[0][q]; }
-      if (pass == 1 && kept) {
-        atomicMax(&s.last, i);
-        if (off + incl > target) atomicMin(&s.tok, i);
-      }
-    }
-    Z = run;
-  }
-  __syncthreads();
-  return s.tok != 0x7fffffff ? s.tok : s.last;
-}
-
 // ---- the kernel -----------------------------------------------------------------------------------------------------
+// Row r is block r; with CL, ranks [0, gridDim.x) of cluster r, each with `per_rank` stretches.
 template <typename T, bool CL>
-__global__ void __launch_bounds__(kMaxWarps * 32) sample_kernel(const Args p, const int per_rank) {
+__global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(const Args p, const int per_rank) {
   pdl_trigger();
   __shared__ Scratch s;
   Group<CL> g{s, (int)threadIdx.x, (int)threadIdx.x & 31, (int)threadIdx.x >> 5, (int)blockDim.x >> 5, CL ? (int)blockIdx.x : 0, CL ? (int)gridDim.x : 1};
   const int threads = blockDim.x;
   const int64_t row = CL ? blockIdx.y : blockIdx.x;
-  Scratch& lead = *(CL ? cooperative_groups::this_cluster().map_shared_rank(&s, 0) : &s);      // the rank that keeps the candidates
-  const int id0 = g.rank * per_rank + g.warp * kWarpIds, end = min(p.V, (g.rank + 1) * per_rank);
+  Scratch& lead = *(CL ? cooperative_groups::this_cluster().map_shared_rank(&s, 0) : &s);      // the rank that keeps the list
+  const int stretches = (p.V + kStretch - 1) / kStretch;
+  const int q0 = CL ? g.rank * per_rank : 0, q1 = CL ? min(stretches, q0 + per_rank) : stretches;
   const T* lr = static_cast<const T*>(p.logits) + row * p.stride;
+  const bool wide = reinterpret_cast<uintptr_t>(lr) % (4 * sizeof(T)) == 0;
   pdl_wait();
 
-  // ---- the row into registers: element (j, e) of a lane is id id0 + 128 j + 4 lane + e ----
-  float w[32];
-  bool odd = false;
-  if (reinterpret_cast<uintptr_t>(lr) % (4 * sizeof(T)) == 0) {
+  // f(logit, id) for this thread's ids of stretch q
+  auto in_stretch = [&](int q, auto&& f) {
+    const int i0 = q * kStretch + 4 * g.lane;
+    float v[16];
+    if (wide && (q + 1) * kStretch <= p.V) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int i = id0 + 128 * j + 4 * g.lane;
-      float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-      if (i + 3 < end) v = ld4(lr + i);
-      else if (i < end) {
-        v.x = to_float(lr[i]);
-        if (i + 1 < end) v.y = to_float(lr[i + 1]);
-        if (i + 2 < end) v.z = to_float(lr[i + 2]);
+      for (int j = 0; j < 4; ++j) {
+        const float4 x = ld4(lr + i0 + 128 * j);
+        v[4 * j] = x.x; v[4 * j + 1] = x.y; v[4 * j + 2] = x.z; v[4 * j + 3] = x.w;
       }
-      w[4 * j] = v.x; w[4 * j + 1] = v.y; w[4 * j + 2] = v.z; w[4 * j + 3] = v.w;
-    }
-  } else {
+    } else {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      const int i = id0 + 128 * (j >> 2) + 4 * g.lane + (j & 3);
-      w[j] = i < end ? to_float(lr[i]) : -INFINITY;
+      for (int j = 0; j < 16; ++j) {
+        const int i = i0 + 128 * (j >> 2) + (j & 3);
+        v[j] = i < p.V ? to_float(lr[i]) : -INFINITY;
+      }
     }
-  }
-  RowArgs a;
-  a.row = row;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) f(v[j], i0 + 128 * (j >> 2) + (j & 3));
+  };
+  auto each = [&](auto&& f) {
+#pragma unroll 1
+    for (int q = q0 + g.warp; q < q1; q += g.warps) in_stretch(q, f);
+  };
+
+  // ---- parameters and the maximum ----
   const float T0 = p.temperature != nullptr ? p.temperature[row] : 1.0f;
   const int k0 = p.top_k != nullptr ? p.top_k[row] : 0;
-  const float p0 = p.top_p != nullptr ? p.top_p[row] : 1.0f, q0 = p.min_p != nullptr ? p.min_p[row] : 0.0f, u0 = p.u[row];
-  a.top_k = k0 <= 0 || k0 > p.V ? p.V : k0;
-  a.top_p = p0 < 1.0f ? (double)fmaxf(p0, 0.0f) : 1.0;
-  a.min_p = q0 > 0.0f ? (double)fminf(q0, 1.0f) : 0.0;
-  a.u = u0 > 0.0f ? (double)u0 : 0.0;
-  float top = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    odd |= !(w[i] < INFINITY);
-    w[i] = w[i] > -INFINITY ? w[i] : -INFINITY;      // (a NaN masks its token)
-    top = fmaxf(top, w[i]);
-  }
+  const float p0 = p.top_p != nullptr ? p.top_p[row] : 1.0f, f0 = p.min_p != nullptr ? p.min_p[row] : 0.0f, u0 = p.u[row];
+  const int top_k = k0 <= 0 || k0 > p.V ? p.V : k0;
+  const double top_p = p0 < 1.0f ? (double)fmaxf(p0, 0.0f) : 1.0, min_p = f0 > 0.0f ? (double)fminf(f0, 1.0f) : 0.0, u = u0 > 0.0f ? (double)u0 : 0.0;
+  float top = -INFINITY;                             // this thread's largest logit
+  bool odd = false;
+  each([&](float l, int) {
+    odd |= !(l < INFINITY);
+    top = fmaxf(top, l);                             // (a NaN masks its token: it fails every comparison)
+  });
   if (odd) raise_status(p.status, kStatusNonFinite);
-  a.l_max = g.max_of(top);
-  if (a.l_max == -INFINITY) {                        // nothing can be picked
+  const float l_max = g.max_of(top);
+  if (l_max == -INFINITY) {                          // nothing can be picked
     if (g.tid == 0 && g.rank == 0) { raise_status(p.status, kStatusNonFinite); p.tok[row] = 0; }
     if (CL) g.sync_all();
     return;
   }
-  auto id_of = [&](int i) { return id0 + 128 * (i >> 2) + 4 * g.lane + (i & 3); };
-  if (!(T0 >= kLeastTemperature) || a.top_k == 1 || a.top_p <= 0.0) {      // the first of the order
+  if (!(T0 >= kLeastTemperature) || top_k == 1 || top_p <= 0.0) {      // the first of the order
     uint32_t best = 0xffffffffu;
-#pragma unroll
-    for (int i = 31; i >= 0; --i) best = w[i] == a.l_max ? (uint32_t)id_of(i) : best;
+    each([&](float l, int id) { best = l == l_max ? min(best, (uint32_t)id) : best; });
     best = g.min_of(best);
     if (g.tid == 0 && g.rank == 0) p.tok[row] = (int)best;
     if (CL) g.sync_all();
     return;
   }
-  a.rate = 1.4426950408889634074 / (double)T0;
-  bool slow = !(T0 <= 1e30f);
-  const float rate = (float)fmin(a.rate, 3e38);
-  // ---- weights ----
-  float mass = 0.f;
-  uint32_t count = 0;
-  const bool need_p = a.top_p < 1.0;
-  bool need_k = a.top_k < p.V;
-  const float least = need_k && need_p ? kLeast : fmaxf(kLeast, (float)a.min_p * (1.0f - kSlack));
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    w[i] = w[i] == a.l_max ? 1.0f : ex2((w[i] - a.l_max) * rate);
-    w[i] = w[i] >= kLeast ? w[i] : 0.0f;             // (and an infinite maximum leaves zeros)
-    mass += w[i];
-    count += w[i] >= least ? 1u : 0u;
+  const double rate64 = 1.4426950408889634074 / (double)T0;            // 1 / (T ln 2)
+  const float rate = (float)fmin(rate64, 3e38);
+  auto weight = [&](float l) { return l == l_max ? 1.0f : ex2(fmaxf(l - l_max, -3e38f) * rate); };
+  auto weight_of = [&](float l) { return weight64(l, l_max, rate64); };
+  // the logit with weight 2^x, as a finite float
+  auto logit_at = [&](double x) {
+    const double v = (double)l_max + x / rate64;
+    return v > -3.4e38 ? (float)v : -3.402823466e38f;
+  };
+  const bool limit_k = top_k < p.V, limit_p = top_p < 1.0;
+  const float least = l_max == INFINITY ? INFINITY : logit_at(kLeastLog2);
+  // min_p as logits: surely below, surely above
+  float floor_lo = least, floor_hi = least;
+  if (min_p > 0.0 && l_max < INFINITY) {
+    const double v = (double)l_max + log2(min_p) / rate64, off = 1e-6 * (fabs(v) + fabs((double)l_max));
+    floor_lo = fmaxf(least, v - off > -3.4e38 ? (float)(v - off) : least);
+    floor_hi = fmaxf(least, v + off > -3.4e38 ? (float)(v + off) : least);
   }
-  g.add(mass, count);
-  const float Z = mass;                              // of the whole row
-  const uint32_t in_all = count;
 
-  auto probe = [&](float t) {
-    mass = 0.f;
-    count = 0;
+  // ---- thresholds lo < hi: {l >= lo} holds all that is kept, {l >= hi} is kept (above min_p); counts and masses ----
+  const float beyond = INFINITY;                     // hi: nothing lies above it (l_max of infinity is told apart by `whole`)
+  float lo = least, hi = beyond, m_lo = 0.f, m_hi = 0.f, Z = 0.f;
+  uint32_t n_lo = 0xffffffffu, n_hi = 0;
+  double all64 = 0.0, above64 = 0.0;
+  bool whole = true;                                 // the list holds every token from l_max down to lo
+  float m3[3];
+  uint32_t n3[3];
+  double x3[3];
+  // Counts and masses at or above three thresholds t3[0] >= t3[1] >= t3[2], and the mass of everything.
+  float t3[3];
+  auto sum3 = [&](bool exact) {
+    double all = 0.0;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      mass += w[i] >= t ? w[i] : 0.f;
-      count += w[i] >= t ? 1u : 0u;
+    for (int i = 0; i < 3; ++i) { m3[i] = 0.f; n3[i] = 0u; x3[i] = 0.0; }
+    float z = 0.f;
+    if (!exact) {
+      each([&](float l, int) {
+        const float w = l >= least ? weight(l) : 0.f;
+        z += w;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (l >= t3[i]) { m3[i] += w; ++n3[i]; }
+      });
+    } else {
+      each([&](float l, int) {
+        if (l >= least) {
+          const double w = weight_of(l);
+          all += w;
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            if (l >= t3[i]) { x3[i] += w; ++n3[i]; }
+        }
+      });
+      all64 = g.add64(all);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) x3[i] = g.add64(x3[i]);
     }
-    g.add(mass, count);
-  };
-
-  // ---- thresholds lo < hi: {w >= lo} holds all that is kept, all of {w >= hi} is kept; n_*, m_* their counts and masses ----
-  float lo = least, hi = 2.0f, m_lo = Z, m_hi = 0.f;
-  uint32_t n_lo = in_all, n_hi = 0;
-  // Narrows [lo, hi) to at most kCap tokens, or down to the first kCap of the order (hi = 2). by_count: the border is the want_n-th
-  // token; else where the mass reaches want_m.
-  auto search = [&](bool by_count, uint32_t want_n, float want_m) {
-    const float sure = want_m * (1.0f + kSlack) + Z * kSlack, unsure = want_m * (1.0f - kSlack) - Z * kSlack;
-    uint32_t between_lo = 0, between_hi = 0;         // bits of thresholds that are neither
-    for (int it = 0; it < kProbes; ++it) {
-      if (n_lo <= (uint32_t)kCap) { hi = 2.0f; n_hi = 0; m_hi = 0.f; return true; }
-      if (n_lo - n_hi <= (uint32_t)kCap && (n_hi > (uint32_t)kCap / 2 || it > 12)) return true;
-      const uint32_t b_lo = __float_as_uint(lo), b_hi = __float_as_uint(hi);
-      uint32_t b;
-      if (between_lo != 0u) {
-        b = (it & 1) ? b_lo + (between_lo - b_lo) / 2 : between_hi + (b_hi - between_hi) / 2;
-      } else if (hi > 1.5f) {                        // nothing known above: down from 2^-6 in steps that double
-        b = it == 0 && lo < 0.0078125f ? __float_as_uint(0.015625f) : b_lo + (b_hi - b_lo) / 2;
-      } else if (lo <= least && lo < 1e-12f) {       // nothing known below
-        const uint32_t d = __float_as_uint(1.0f) - b_hi;
-        b = max(b_hi - max(d, 1u << 24), b_lo + (b_hi - b_lo) / 8);
-      } else {                                       // by interpolation between the two, or halfway, in turn
-        float f = by_count ? ((float)want_n - (float)n_hi) / ((float)n_lo - (float)n_hi) : (want_m - m_hi) / (m_lo - m_hi);
-        f = (it & 1) ? 0.5f : fminf(fmaxf(f, 0.1f), 0.9f);
-        b = b_hi - (uint32_t)((float)(b_hi - b_lo) * f);
-      }
-      if (b <= b_lo || b >= b_hi) break;
-      const float t = __uint_as_float(b);
-      probe(t);
-      const bool enough = by_count ? count >= want_n : mass >= sure, few = by_count ? count < want_n : mass < unsure;
-      if (enough) { lo = t; n_lo = count; m_lo = mass; if (between_lo != 0u && between_lo <= b) between_lo = between_hi = 0u; }
-      else if (few) { hi = t; n_hi = count; m_hi = mass; if (between_hi != 0u && between_hi >= b) between_lo = between_hi = 0u; }
-      else {
-        between_lo = between_lo == 0u ? b : min(between_lo, b);
-        between_hi = max(between_hi, b);
-      }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) g.add(m3[i], n3[i]);
+    uint32_t none = 0;
+    if (!exact) {
+      g.add(z, none);
+      Z = z;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) x3[i] = (double)m3[i];
     }
-    return n_lo - n_hi <= (uint32_t)kCap;
   };
-  // The tokens of [lo, hi) as sorted words with weights and running sums, in the leading rank.
+  // Takes over what a threshold says. by_count: the border is token want_n of the order; else where the mass reaches want.
+  auto place = [&](bool by_count, uint32_t want_n, double want, double slack, double total) {
+#pragma unroll
+    for (int i = 2; i >= 0; --i) {
+      const bool enough = by_count ? n3[i] >= want_n : x3[i] >= want + (want + total) * slack;
+      const bool few = by_count ? n3[i] < want_n : x3[i] < want - (want + total) * slack;
+      if (enough && t3[i] >= lo) { lo = t3[i]; n_lo = n3[i]; m_lo = (float)x3[i]; }
+      if (few && t3[i] < hi) { hi = t3[i]; n_hi = n3[i]; m_hi = (float)x3[i]; }
+    }
+  };
+  // Closes in until the first kCap of the order reach the border (whole), or at most kCap tokens lie between lo and hi. False: the
+  // border lies in a group of equal logits, all that is left between lo and hi; or (not exact) among too many tokens for the bounds.
+  auto search = [&](bool by_count, uint32_t want_n, double want, bool exact) {
+    const double slack = exact ? kSlack64 : (double)kSlack;
+    double down = 4.0;                               // octaves below the maximum, while nothing is known below
+    for (int it = 0; it < kRounds; ++it) {
+      if (n_lo <= (uint32_t)kCap) { whole = true; return true; }
+      if (n_lo != 0xffffffffu && n_lo - n_hi <= (uint32_t)kCap && (n_hi > (uint32_t)kCap / 2 || it > 4)) { whole = false; return true; }
+      const bool unbounded = n_lo == 0xffffffffu;
+      const uint32_t k_lo = logit_key(lo), k_hi = hi < beyond ? logit_key(hi) : logit_key(l_max) + 1u;
+      if (!unbounded && k_hi - k_lo <= 1u) break;
+      if (unbounded) {                               // down from the top in growing steps
+        t3[0] = it == 0 ? l_max : fmaxf(least, logit_at(-down));
+        t3[1] = fmaxf(least, logit_at(-1.5 * down));
+        t3[2] = it >= 8 ? least : fmaxf(least, logit_at(-2.25 * down));
+        down *= it == 0 ? 2.25 : 3.375;
+      } else if ((it & 1) && hi < beyond) {          // around an estimate
+        float c = by_count ? ((float)want_n - (float)n_hi) / ((float)n_lo - (float)n_hi) : ((float)want - m_hi) / (m_lo - m_hi);
+        c = fminf(fmaxf(c, 0.08f), 0.92f);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) t3[i] = (float)((double)hi - ((double)hi - (double)lo) * (double)(c + 0.06f * (float)(i - 1)));
+      } else {                                       // at quarters of the keys
+        const uint32_t d = k_hi - k_lo;
+        t3[0] = key_logit(k_hi - max(d / 4, 1u));
+        t3[1] = key_logit(k_lo + d / 2);
+        t3[2] = key_logit(k_lo + max(d / 4, 1u));
+      }
+      const bool quarters = !unbounded && !((it & 1) && hi < beyond);
+      const float lo_was = lo, hi_was = hi;
+      sum3(exact);
+      place(by_count, want_n, want, slack, exact ? all64 : (double)Z);
+      if (unbounded && n_lo == 0xffffffffu && t3[2] <= least) { lo = least; n_lo = n3[2]; m_lo = (float)x3[2]; }
+      if (!exact && !by_count && quarters && lo == lo_was && hi == hi_was) break;
+    }
+    whole = false;
+    return n_lo != 0xffffffffu && n_lo - n_hi <= (uint32_t)kCap;
+  };
+  // The tokens of [lo, hi) as sorted words with weights and running sums, in the leading rank; all ranks get their number.
   int n = 0;
-  auto gather = [&]() {
+  auto collect_begin = [&]() {
     if (g.tid == 0) s.count = 0;
     g.sync_all();
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (w[i] >= lo && w[i] < hi) {
-        const uint32_t at = atomicAdd(&lead.count, 1u);
-        if (at < (uint32_t)kCap) lead.cand[at] = (unsigned long long)id_of(i);
-      }
+  };
+  auto collect = [&](float l, int id) {
+    const uint32_t at = atomicAdd(&lead.count, 1u);
+    if (at < (uint32_t)kCap) lead.cand[at] = word_of(l, id);
+  };
+  auto collect_end = [&]() {
     g.sync_all();
+    n = (int)min(lead.count, (uint32_t)kCap + 1u);
+    g.sync_all();
+    return (uint32_t)n;
+  };
+  auto order = [&]() {                               // (after collect_end, at most kCap)
     if (g.rank != 0) return;
-    n = (int)min(s.count, (uint32_t)kCap);
-    for (int i = g.tid; i < n; i += threads) s.cand[i] = word_of(to_float(lr[s.cand[i]]), (int)s.cand[i]);
-    __syncthreads();
-    sort_words(s.cand, n, g.tid, threads);
-    for (int i = g.tid; i < n; i += threads) s.weight[i] = weight64(word_logit(s.cand[i]), a.l_max, a.rate);
+    unsigned long long* other = reinterpret_cast<unsigned long long*>(s.run);
+    if (n <= 192) {
+      sort_short(s.cand, other, n, g.tid, threads);
+      for (int i = g.tid; i < n; i += threads) {
+        const unsigned long long w = other[i];
+        s.cand[i] = w;
+        s.weight[i] = weight_of(word_logit(w));
+      }
+    } else {
+      sort_words(s.cand, n, g.tid, threads);
+      for (int i = g.tid; i < n; i += threads) s.weight[i] = weight_of(word_logit(s.cand[i]));
+    }
     __syncthreads();
     running_sums(s.weight, s.run, n, g.tid, threads, s.d[0]);
   };
-  // Sums in 64 bits over the row's own logits: of all weights, and of those at or above hi (also per warp, in the leading rank).
-  double all64 = 0.0, above64 = 0.0;
-  auto weigh = [&](bool whole) {
-    double x = 0.0, y = 0.0;
-#pragma unroll 4
-    for (int i = 0; i < 32; ++i) {
-      const int id = id_of(i);
-      if (id >= end) continue;
-      const float l = to_float(lr[id]);
-      if (!(l > -INFINITY)) continue;
-      const float wf = l == a.l_max ? 1.0f : ex2((l - a.l_max) * rate);
-      const bool over = wf >= hi && wf >= kLeast;
-      if (!over && !whole) continue;
-      const double v = weight64(l, a.l_max, a.rate);
-      x += v;
-      y += over ? v : 0.0;
-    }
-    y = warp_sum64(y);
-    if (g.lane == 0) lead.warp_sum[id0 / kWarpIds] = y;
-    above64 = g.add64(g.lane == 0 ? y : 0.0);
-    if (whole) all64 = g.add64(x);
+  auto gather = [&]() {
+    collect_begin();
+    each([&](float l, int id) {
+      if (l >= lo && (whole || l < hi)) collect(l, id);
+    });
+    return collect_end();
   };
-  // How many of the gathered tokens are kept (leading rank). k_left: places that top_k leaves them; want: the mass that ends the
-  // nucleus, counted from `before` on; limit: only words up to it. unsure: how far `want` may be off.
-  auto decide = [&](int k_left, bool by_mass, double want, double before, unsigned long long limit, double off, bool floor_p, int* unsure) {
+  // Sums in 64 bits: of the tokens that `kept` takes, also per stretch (in the leading rank), and, with all, of everything.
+  auto weigh = [&](bool all, auto&& kept) {
+    double x = 0.0, y = 0.0;
+#pragma unroll 1
+    for (int q = q0 + g.warp; q < q1; q += g.warps) {
+      double in = 0.0;
+      in_stretch(q, [&](float l, int id) {
+        const bool k = l >= least && kept(l, id);
+        if (k || (all && l >= least)) {
+          const double w = weight_of(l);
+          x += w;
+          in += k ? w : 0.0;
+        }
+      });
+      in = warp_sum64(in);
+      y += in;
+      if (g.lane == 0) lead.part[q] = in;
+    }
+    above64 = g.add64(g.lane == 0 ? y : 0.0);
+    if (all) all64 = g.add64(x);
+  };
+  // How many of the list are kept (leading rank): the first k_left, words up to `limit`, what begins below the mass `want`
+  // (counted from `before` on), and what has min_p. *unsure: a border closer to `want` than `off`.
+  auto decide = [&](int k_left, bool by_mass, double want, double before, unsigned long long limit, double off, bool by_floor, int* unsure) {
     if (g.tid == 0) { s.keep = 0; s.unsure = 0; }
     __syncthreads();
     int mine = 0, doubt = 0;
     for (int i = g.tid; i < n; i += threads) {
       const double b = before + (i > 0 ? s.run[i - 1] : 0.0);
-      const bool in = i < k_left && s.cand[i] <= limit && (!floor_p || s.weight[i] >= a.min_p);
-      const bool first = i == 0 && before == 0.0;
+      const bool in = i < k_left && s.cand[i] <= limit && (!by_floor || s.weight[i] >= min_p), first = i == 0 && before == 0.0;
       mine += in && (!by_mass || first || b < want) ? 1 : 0;
       doubt |= by_mass && in && !first && fabs(b - want) <= off ? 1 : 0;
     }
@@ -539,193 +511,303 @@ __global__ void __launch_bounds__(kMaxWarps * 32) sample_kernel(const Args p, co
     __syncthreads();
     return keep;
   };
+  // From the leading rank to all.
+  auto tell = [&](double a, double b, double& x, double& y) {
+    __syncthreads();
+    if (g.tid == 0 && g.rank == 0) { s.box[0] = a; s.box[1] = b; }
+    g.sync_all();
+    x = lead.box[0];
+    y = lead.box[1];
+    g.sync_all();
+  };
 
-  int keep = 0;
+  // ---- which tokens the border lies among ----
+  bool by_k = limit_k, by_mass = limit_p, listed = false, tie = false, all_kept = false;
   unsigned long long border = ~0ull;                 // words up to it are kept
-  double mass_k = -1.0;                              // mass of the first top_k, where a list gave it
-  if (!slow && need_k && in_all > (uint32_t)a.top_k && in_all > (uint32_t)kCap) {
-    bool found = false;
-    if (!CL && a.top_k <= 256 && 2 * a.top_k <= threads) {
-      // The top_k-th largest of the threads' maxima, 16 bits of it: at least top_k weights are as large, and few more.
-      float mx = 0.f;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) mx = fmaxf(mx, w[i]);
-      const uint32_t bits = __float_as_uint(mx);
-      uint32_t t = 0;
-      for (int b = 29; b >= 14; --b)
-        if (__syncthreads_count(bits >= (t | (1u << b))) >= a.top_k) t |= 1u << b;
-      const float tf = __uint_as_float(t);
-      if (tf > lo) {
-        probe(tf);
-        if (count <= (uint32_t)kCap && count >= (uint32_t)a.top_k) { lo = tf; n_lo = count; m_lo = mass; found = true; }
+  double mass_k = -1.0;                              // mass of the first top_k, once known
+  const int guess = limit_k ? top_k : 64;            // a threshold that about so many tokens reach
+  float first = -INFINITY;
+  if ((limit_k || limit_p) && 2 * guess <= threads) {
+    const uint32_t key = logit_key(top);
+    uint32_t t = 0;
+    for (int b = 31; b >= 16; --b)                   // 16 bits of it
+      if (__syncthreads_count(key >= (t | (1u << b))) >= guess) t |= 1u << b;
+    first = t != 0u ? key_logit(t) : -INFINITY;
+    if (CL) first = g.max_of(first);                 // (the rank that has it alone has as many)
+  }
+  const float floor_list = limit_k && limit_p ? least : floor_lo;      // (top_p counts the mass of top_k without regard to min_p)
+  if (limit_k) {
+    if (first > -INFINITY) {
+      lo = fmaxf(first, floor_list);
+      n_lo = gather();
+      listed = n_lo <= (uint32_t)kCap;
+      if (!listed) {                                 // (more than the list counted)
+        if (lo > floor_list) {
+          t3[0] = t3[1] = t3[2] = lo;
+          sum3(false);
+          n_lo = n3[0];
+          m_lo = m3[0];
+        } else {
+          n_lo = 0xffffffffu;
+        }
       }
     }
-    if (!found) found = search(true, (uint32_t)a.top_k, 0.f);
-    slow = !found;
-    if (found && hi < 1.5f && need_p) {
-      // Too many for one list: the border of top_k first, and the mass inside it
+    if (!listed && n_lo == 0xffffffffu) {            // few tokens in all?
+      lo = floor_list;
+      n_lo = gather();
+      listed = n_lo <= (uint32_t)kCap;
+      if (!listed) {
+        t3[0] = t3[1] = t3[2] = lo;
+        sum3(false);
+        n_lo = n3[0];
+        by_k = n_lo >= (uint32_t)top_k;
+        if (by_k) n_lo = 0xffffffffu;                // (the search begins at the top)
+      }
+    }
+    if (!listed && by_k) {
+      tie = !search(true, (uint32_t)top_k, 0.0, false);
+      if (tie && limit_p) {                          // the mass of top_k; its nucleus may end above the equal logits
+        const float v = lo;
+        weigh(false, [&](float l, int) { return l > v; });
+        mass_k = above64 + (double)((uint32_t)top_k - n_hi) * weight_of(v);
+        if (top_p * mass_k <= above64) {
+          tie = by_k = false;
+          hi = beyond; n_hi = 0; m_hi = 0.f;
+        }
+      }
+    }
+    if (!listed && by_k && !tie && !whole && limit_p) {
+      // too many for one list: the border of top_k first, and the mass inside it
       gather();
-      weigh(false);
-      double info[2] = {0.0, 0.0};
+      order();
+      const float above = hi;
+      weigh(false, [&](float l, int) { return l >= above; });
+      double b = 0.0;
       if (g.rank == 0) {
-        keep = decide(a.top_k - (int)n_hi, false, 0.0, above64, ~0ull, 0.0, false, nullptr);
-        info[0] = above64 + s.run[keep - 1];
-        if (CL && g.tid == 0) s.d[0][0] = info[0], s.run[0] = __longlong_as_double((long long)s.cand[keep - 1]);
-        border = s.cand[keep - 1];
-      }
-      if (CL) {
-        g.sync_all();
-        info[0] = lead.d[0][0];
-        border = (unsigned long long)__double_as_longlong(lead.run[0]);
-        g.sync_all();
-      }
-      mass_k = info[0];
-      hi = 2.0f; n_hi = 0; m_hi = 0.f;
-      slow = !search(false, 0, (float)(a.top_p * mass_k));
-      need_k = false;
-    }
-  } else if (need_k && in_all <= (uint32_t)a.top_k) {
-    need_k = false;                                  // top_k ends behind all weights that count
-  }
-  bool k_by_list = need_k && !slow, by_mass = need_p;      // the list holds the border of top_k, of the nucleus
-  if (!slow && !k_by_list && mass_k < 0.0 && in_all > (uint32_t)kCap) {
-    if (need_p) {
-      const float want = (float)a.top_p * Z;
-      // (min_p may end the kept tokens above the nucleus' border: then it alone decides)
-      probe(least);
-      if (mass < want * (1.0f - kSlack) - Z * kSlack) {
-        hi = fmaxf(least, (float)a.min_p * (1.0f + 2.0f * kSlack));
-        probe(hi);
-        n_hi = count;
-        slow = n_lo - n_hi > (uint32_t)kCap;
+        const int keep = decide(top_k - (int)n_hi, false, 0.0, above64, ~0ull, 0.0, false, nullptr);
+        tell(above64 + s.run[keep - 1], __longlong_as_double((long long)s.cand[keep - 1]), mass_k, b);
       } else {
-        m_lo = mass;
-        slow = !search(false, 0, want);
+        tell(0.0, 0.0, mass_k, b);
       }
-    } else {
-      hi = a.min_p > 0.0 ? (float)a.min_p * (1.0f + 2.0f * kSlack) : kLeast;
-      if (a.min_p > 0.0) {
-        probe(hi);
-        n_hi = count;
-        slow = n_lo - n_hi > (uint32_t)kCap;
-      } else {
-        lo = hi;                                     // everything is kept: no list
-        n_hi = n_lo;
-      }
+      border = (unsigned long long)__double_as_longlong(b);
+      by_k = false;
+      hi = beyond; n_hi = 0; m_hi = 0.f;
+      whole = true;
     }
   }
-  if (!slow && a.min_p > 0.0 && hi < (float)a.min_p * (1.0f + 2.0f * kSlack)) {
-    // not all above the border has min_p: it ends the kept tokens by itself, unless both lie within the bounds
-    const float t = (float)a.min_p * (1.0f - 2.0f * kSlack);
-    slow = hi > t;
-    if (!slow) {
-      k_by_list = by_mass = false;
+  if (!listed && !tie && by_mass && !by_k) {
+    double want = top_p * mass_k;
+    bool ok = false;
+    if (mass_k < 0.0) {
+      // the mass of all, and a first list in the same pass
+      t3[0] = fmaxf(first, floor_lo);
+      t3[1] = fmaxf(least, logit_at(-6.0));
+      t3[2] = fmaxf(least, logit_at(-12.0));
+      if (t3[1] > t3[0]) t3[1] = t3[0];
+      if (t3[2] > t3[1]) t3[2] = t3[1];
+      const bool try_list = first > -INFINITY;
+      if (try_list) collect_begin();
+      float z = 0.f, a0 = 0.f, a1 = 0.f, a2 = 0.f;
+      uint32_t c0 = 0, c1 = 0, c2 = 0;
+      each([&](float l, int id) {
+        const float w = l >= least ? weight(l) : 0.f;
+        z += w;
+        if (l >= t3[2]) { a2 += w; ++c2; }
+        if (l >= t3[1]) { a1 += w; ++c1; }
+        if (l >= t3[0]) { a0 += w; ++c0; if (try_list) collect(l, id); }
+      });
+      uint32_t none = 0;
+      g.add(z, none);
+      g.add(a0, c0); g.add(a1, c1); g.add(a2, c2);
+      Z = z;
+      m3[0] = a0; m3[1] = a1; m3[2] = a2;
+      n3[0] = c0; n3[1] = c1; n3[2] = c2;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) x3[i] = (double)m3[i];
+      want = top_p * (double)Z;
+      place(false, 0, want, (double)kSlack, (double)Z);
+      // the first list serves if the nucleus, or min_p, ends inside it
+      if (try_list && n3[0] <= (uint32_t)kCap && (lo >= t3[0] || t3[0] <= floor_lo)) {
+        lo = t3[0];
+        n_lo = n3[0];
+        listed = true;
+        collect_end();
+      } else if (try_list) {
+        collect_end();
+      }
+    }
+    if (!listed) {
+      ok = search(false, 0, want, false);
+      if (!ok) {                                     // too many tokens within the bounds: the same in 64 bits
+        lo = least; hi = beyond; n_lo = 0xffffffffu; n_hi = 0; m_hi = 0.f;
+        if (mass_k < 0.0) {
+          weigh(true, [&](float, int) { return true; });
+          mass_k = all64;
+          want = top_p * all64;
+        }
+        ok = search(false, 0, want, true);
+        tie = !ok;
+      }
+    }
+  }
+  bool floor_later = false;
+  if (!listed && !tie && !by_k && !by_mass) {
+    if (min_p > 0.0) {
+      lo = floor_lo;
+      listed = gather() <= (uint32_t)kCap;
+    }
+    all_kept = !listed;                              // down to min_p
+  } else if (!listed && !tie && !whole && min_p > 0.0 && hi < floor_hi) {
+    // not everything above the border has min_p
+    if (hi <= floor_lo) {
+      all_kept = true;                               // min_p ends the kept tokens above it
       border = ~0ull;
-      lo = t;
-      probe(lo);
-      n_lo = count;
-      hi = 2.0f;
-      n_hi = 0;
-      if (n_lo > (uint32_t)kCap) {
-        hi = (float)a.min_p * (1.0f + 2.0f * kSlack);
-        probe(hi);
-        n_hi = count;
-        slow = n_lo - n_hi > (uint32_t)kCap;
-      }
+    } else {
+      floor_later = true;                            // both lie within the bounds of each other
     }
   }
-  if (slow) {
-    if (CL) g.sync_all();
+
+  // ---- the border, and how many of the list are kept ----
+  int keep = 0;
+  unsigned long long upto = ~0ull;                   // without a list: words up to it are kept, down to min_p
+  if (!tie && !all_kept) {
+    whole = whole || listed;
+    if (whole) n_hi = 0;
+    if (!listed) gather();
+    order();
+    const float above = hi;
+    const bool sums = !whole;
+    if (sums) weigh(by_mass && mass_k < 0.0, [&](float l, int) { return l >= above; });
+    const int k_left = by_k ? top_k - (int)n_hi : n;
+    const bool by_floor = min_p > 0.0 && !floor_later;
+    double doubt = 0.0, word = 0.0;
     if (g.rank == 0) {
-      const int tok = slow_row<T>(p, a, s);
-      if (g.tid == 0) p.tok[row] = tok;
+      if (by_k && by_mass && whole) mass_k = s.run[min(k_left, n) - 1];
+      const bool rough = by_mass && mass_k < 0.0 && whole;
+      const double total = mass_k >= 0.0 ? mass_k : whole ? (double)Z : all64;
+      int d = 0;
+      keep = decide(k_left, by_mass, top_p * total, sums ? above64 : 0.0, border, rough ? 2.0 * (double)kSlack * (double)Z : 0.0, by_floor, &d);
+      doubt = (double)d;
+      word = __longlong_as_double((long long)(keep > 0 ? s.cand[keep - 1] : word_of(hi, 0) | 0xffffffffull));
     }
-    return;
-  }
-  const bool whole_list = hi > 1.5f;
-  gather();
-  if (!whole_list) weigh(by_mass && mass_k < 0.0);
-  // ---- the border, and which of the gathered tokens are kept ----
-  if (g.rank == 0) {
-    const int k_left = k_by_list ? a.top_k - (int)n_hi : n;
-    if (k_by_list && by_mass && whole_list) mass_k = s.run[min(k_left, n) - 1];
-    const double total = mass_k >= 0.0 ? mass_k : !whole_list ? all64 : (double)Z;
-    const bool rough = by_mass && mass_k < 0.0 && whole_list;
-    int doubt = 0;
-    keep = decide(k_left, by_mass, a.top_p * total, whole_list ? 0.0 : above64, border, rough ? 2.0 * kSlack * Z : 0.0, a.min_p > 0.0, &doubt);
-    if (CL && g.tid == 0) s.keep = doubt;
-    if (CL) __syncthreads();
-    if (!CL && doubt) {                              // the fp32 total is not enough
-      weigh(true);
-      keep = decide(k_left, by_mass, a.top_p * all64, 0.0, border, 0.0, a.min_p > 0.0, nullptr);
+    if (CL) tell(doubt, word, doubt, word);
+    if (doubt != 0.0) {                              // the fp32 total is not enough
+      weigh(true, [&](float, int) { return false; });
+      if (g.rank == 0) keep = decide(k_left, by_mass, top_p * all64, 0.0, border, 0.0, by_floor, nullptr);
     }
-  }
-  if (CL) {
+    upto = (unsigned long long)__double_as_longlong(word);
+  } else if (tie) {
+    // More equal logits than the list holds: all between lo and hi are one value v, and the border is the m-th of them by id.
+    const float v = lo;
+    weigh(by_mass && mass_k < 0.0, [&](float l, int) { return l > v; });
+    const double above_v = above64, w = weight_of(v), total = mass_k >= 0.0 ? mass_k : all64;
+    uint32_t left = 0xffffffffu;
+    if (by_k) left = (uint32_t)top_k - n_hi;
+    if (by_mass) {                                   // the first c >= 1 with above_v + c w >= want
+      const double want = top_p * total;
+      double c = w > 0.0 ? ceil((want - above_v) / w) : 1.0;
+      if (c > 1.0 && above_v + (c - 1.0) * w >= want) c -= 1.0;
+      if (above_v + c * w < want) c += 1.0;
+      c = fmax(c, 1.0);
+      left = c < (double)left ? (uint32_t)c : left;
+    }
+    // the id of that one: ties per stretch, the stretch, the place in it
+#pragma unroll 1
+    for (int q = q0 + g.warp; q < q1; q += g.warps) {
+      uint32_t c = 0;
+      in_stretch(q, [&](float l, int) { c += l == v ? 1u : 0u; });
+      c = __reduce_add_sync(0xffffffffu, c);
+      if (g.lane == 0) lead.ties[q] = c;
+    }
     g.sync_all();
-    const int doubt = lead.keep;
-    g.sync_all();
-    if (doubt) {
-      weigh(true);
-      if (g.rank == 0) keep = decide(k_by_list ? a.top_k - (int)n_hi : n, by_mass, a.top_p * all64, 0.0, border, 0.0, a.min_p > 0.0, nullptr);
-    } else if (!whole_list) {
-      g.sync_all();                                  // (the warps' sums are in the leading rank)
+    double id = -1.0, unused = 0.0;                  // (none: they are fewer, and all kept)
+    if (g.rank == 0 && g.warp == 0) {
+      int at = -1;
+      for (int q = 0; q < stretches && at < 0; ++q) {
+        if (s.ties[q] >= left) at = q;
+        else left -= s.ties[q];
+      }
+      if (at >= 0)
+        for (int i0 = at * kStretch; i0 < (at + 1) * kStretch && id < 0.0; i0 += 32) {
+          const uint32_t bal = __ballot_sync(0xffffffffu, i0 + g.lane < p.V && to_float(lr[min(i0 + g.lane, p.V - 1)]) == v);
+          if ((uint32_t)__popc(bal) >= left) id = (double)(i0 + (int)__fns(bal, 0, (int)left));
+          else left -= __popc(bal);
+        }
     }
-    if (g.rank != 0) { g.sync_all(); return; }
+    tell(id, 0.0, id, unused);
+    upto = word_of(v, id >= 0.0 ? (int)id : -1);
   }
+  const bool from_list = !tie && !all_kept && !floor_later;
+  if (!from_list) {
+    // masses kept per stretch
+    upto = upto < border ? upto : border;
+    const bool by_floor = min_p > 0.0;
+    weigh(false, [&](float l, int i) { return word_of(l, i) <= upto && (!by_floor || l >= floor_hi || (l >= floor_lo && weight_of(l) >= min_p)); });
+  }
+  if (CL && g.rank != 0) { g.sync_all(); return; }
 
   // ---- the draw (leading rank) ----
-  if (whole_list && keep <= 128) {
+  if (from_list && whole && keep <= 192) {
+    // cumulative masses by id, eight lanes per token
     if (g.tid == 0) { s.tok = 0x7fffffff; s.last = -1; }
     __syncthreads();
-    for (int i = g.tid; i < keep; i += threads) {
-      const uint32_t id = (uint32_t)s.cand[i];
-      double c = 0.0, z = 0.0;
-      for (int j = 0; j < keep; ++j) {
-        const double x = s.weight[j];
-        z += x;
-        c += (uint32_t)s.cand[j] <= id ? x : 0.0;
+    for (int c0 = 0; c0 < keep; c0 += threads >> 3) {
+      const int c = c0 + (g.tid >> 3);
+      const uint32_t id = c < keep ? (uint32_t)s.cand[c] : 0u;
+      double in = 0.0, z = 0.0;
+      for (int j = g.tid & 7; j < keep; j += 8) {
+        const double w = s.weight[j];
+        z += w;
+        in += (uint32_t)s.cand[j] <= id ? w : 0.0;
       }
-      atomicMax(&s.last, (int)id);
-      if (c > a.u * z) atomicMin(&s.tok, (int)id);
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) {
+        z += __shfl_xor_sync(0xffffffffu, z, o);
+        in += __shfl_xor_sync(0xffffffffu, in, o);
+      }
+      if (c < keep && (g.tid & 7) == 0) {
+        atomicMax(&s.last, (int)id);
+        if (in > u * z) atomicMin(&s.tok, (int)id);
+      }
     }
     __syncthreads();
     if (g.tid == 0) p.tok[row] = s.tok != 0x7fffffff ? s.tok : s.last;
   } else {
-    // masses per stretch of 1024 ids, the stretch that u falls in, and its ids one after the other
-    const int stretches = (p.V + kWarpIds - 1) / kWarpIds;
-    for (int q = g.warp; q < stretches; q += g.warps) {
-      double x = 0.0;
-      for (int i = g.lane; i < keep; i += 32) x += ((uint32_t)s.cand[i] >> 10) == (uint32_t)q ? s.weight[i] : 0.0;
-      x = warp_sum64(x);
-      if (g.lane == 0) s.warp_sum[q] = (whole_list ? 0.0 : s.warp_sum[q]) + x;
+    // masses per stretch, the stretch that u falls in, and its ids one after the other
+    if (from_list) {
+      upto = keep > 0 ? s.cand[keep - 1] : 0ull;
+      for (int q = g.warp; q < stretches; q += g.warps) {
+        double x = 0.0;
+        for (int i = g.lane; i < keep; i += 32) x += (uint32_t)s.cand[i] / kStretch == (uint32_t)q ? s.weight[i] : 0.0;
+        x = warp_sum64(x);
+        if (g.lane == 0) s.part[q] = (whole ? 0.0 : s.part[q]) + x;
+      }
     }
     __syncthreads();
     if (g.warp == 0) {
       double z = 0.0;
-      for (int q = 0; q < stretches; ++q) z += s.warp_sum[q];
-      const double target = a.u * z;
+      for (int q = 0; q < stretches; ++q) z += s.part[q];
+      const double target = u * z;
       double run = 0.0;
       int at = -1, last = 0;
       for (int q = 0; q < stretches && at < 0; ++q) {
-        const double x = s.warp_sum[q];
+        const double x = s.part[q];
         if (x > 0.0) last = q;
         if (run + x > target) at = q;
         else run += x;
       }
-      // (rounding may put u behind the last stretch: the last token kept then)
-      const bool past = at < 0;
+      const bool past = at < 0;                      // (rounding put u behind the last stretch: the last token kept then)
       if (past) at = last;
-      const unsigned long long upto = keep > 0 ? s.cand[keep - 1] : 0ull;      // last word kept of the list
       int tok = -1, end_tok = -1;
-      for (int i0 = at * kWarpIds; i0 < min(p.V, (at + 1) * kWarpIds) && tok < 0; i0 += 32) {
+      for (int i0 = at * kStretch; i0 < min(p.V, (at + 1) * kStretch) && tok < 0; i0 += 32) {
         const int id = i0 + g.lane;
         double x = 0.0;
         if (id < p.V) {
           const float l = to_float(lr[id]);
-          if (l > -INFINITY) {
-            const float wf = l == a.l_max ? 1.0f : ex2((l - a.l_max) * rate);
-            const bool kept = wf >= kLeast && (wf >= hi || (keep > 0 && wf >= lo && word_of(l, id) <= upto));
-            if (kept) x = weight64(l, a.l_max, a.rate);
+          const bool over = from_list && !whole && l >= hi;
+          if (l >= least && (over || word_of(l, id) <= upto)) {
+            x = weight_of(l);
+            if (!from_list && !(x >= min_p)) x = 0.0;
           }
         }
         double incl = x;
