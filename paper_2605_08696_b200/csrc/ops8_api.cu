@@ -139,13 +139,13 @@ int launch_sample(const smp::Args& p, cudaStream_t st) {
   const int stretches = (p.V + smp::kStretch - 1) / smp::kStretch;
   ++g_kernel_launches;
   int ranks = 1;
-  while (ranks < smp::kMaxRanks && stretches > 64 * ranks && 2 * ranks * p.R <= sms) ranks *= 2;
+  while (ranks < smp::kMaxRanks && stretches > 32 * ranks && 2 * ranks * p.R <= sms) ranks *= 2;
   if (ranks == 1) {
     const int warps = stretches < 16 ? stretches : 16;
     SRM_CUDA(launch_kernel(smp::sample_kernel<T, false>, dim3((unsigned)p.R), dim3(32 * warps), 0, st, p, stretches));
     return SRM_OK;
   }
-  const int per_rank = (stretches + ranks - 1) / ranks, warps = per_rank < smp::kMaxWarps ? per_rank : smp::kMaxWarps;
+  const int per_rank = (stretches + ranks - 1) / ranks, warps = per_rank < 16 ? per_rank : 16;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ranks, (unsigned)p.R);                  // (few rows)
   cfg.blockDim = dim3(32 * warps);

@@ -144,6 +144,14 @@ struct Group {
     }
     return v;
   }
+  __device__ uint32_t block_max(uint32_t v) {                          // (of this block alone)
+    const int b = turn;
+    turn ^= 1;
+    v = __reduce_max_sync(0xffffffffu, v);
+    if (lane == 0) s.n[b][warp] = v;
+    __syncthreads();
+    return __reduce_max_sync(0xffffffffu, lane < warps ? s.n[b][lane] : 0u);
+  }
   __device__ uint32_t min_of(uint32_t v) {
     const int b = turn;
     turn ^= 1;
@@ -248,10 +256,106 @@ __device__ inline void running_sums(const double* d, double* run, int n, int tid
   __syncthreads();
 }
 
+// largest of three, NaN if one of them is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// A list of at most 32 R tokens that holds all that is kept, from order to token, by one warp: place e of the order is register
+// e / 32 of lane e % 32. (As steps of the block, a barrier and more between each two, the same took four times as long and fifteen
+// warps' issue slots with it.) total: the mass that top_p counts, negative: that of the first k_left. Returns -1 when a border lies
+// closer to the nucleus' mass than `off`.
+template <int R, typename W>
+__device__ __noinline__ int short_list(const unsigned long long* list, int n, int k_left, bool by_mass, double top_p, double total, double off,
+                                       unsigned long long limit, double min_p, double u, int lane, W weight_of) {
+  unsigned long long w[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) w[r] = 32 * r + lane < n ? list[32 * r + lane] : ~0ull;
+#pragma unroll 1
+  for (int size = 2; size <= 32 * R; size <<= 1) {
+#pragma unroll
+    for (int d = R / 2; d > 0; d >>= 1)              // places 32 d apart: other registers of the lane
+      if (size > 32 * d) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if ((r & d) == 0) {
+            const bool up = ((32 * r) & size) == 0;
+            const unsigned long long x = w[r], y = w[r + d];
+            if ((x > y) == up) { w[r] = y; w[r + d] = x; }
+          }
+      }
+#pragma unroll 1
+    for (int d = min(size >> 1, 16); d > 0; d >>= 1) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const unsigned long long y = __shfl_xor_sync(0xffffffffu, w[r], d);
+        const bool up = ((32 * r + lane) & size) == 0, low = (lane & d) == 0;
+        w[r] = (w[r] > y) == (up == low) ? y : w[r];
+      }
+    }
+  }
+  double x[R], before[R];
+  double run = 0.0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    x[r] = 32 * r + lane < n ? weight_of(word_logit(w[r])) : 0.0;
+    double incl = x[r];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    const double prev = __shfl_up_sync(0xffffffffu, incl, 1);
+    before[r] = run + (lane == 0 ? 0.0 : prev);
+    if (total < 0.0 && by_mass) {                    // up to place k_left - 1
+      const int last = min(k_left, n) - 1;
+      const double t = __shfl_sync(0xffffffffu, run + incl, last & 31);
+      if (last >> 5 == r) total = t;
+    }
+    run += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  const double want = top_p * total;
+  int keep = 0;
+  bool doubt = false;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int e = 32 * r + lane;
+    const bool in = e < k_left && e < n && w[r] <= limit && (!(min_p > 0.0) || x[r] >= min_p);
+    keep += __popc(__ballot_sync(0xffffffffu, in && (!by_mass || e == 0 || before[r] < want)));
+    doubt |= by_mass && in && e > 0 && fabs(before[r] - want) < off;
+  }
+  if (__any_sync(0xffffffffu, doubt)) return -1;
+  double z = 0.0, c[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) c[r] = 0.0;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll 2
+    for (int j = 0; j < min(32, keep - 32 * r); ++j) {
+      const uint32_t id = __shfl_sync(0xffffffffu, (uint32_t)w[r], j);
+      const double y = __shfl_sync(0xffffffffu, x[r], j);
+      z += y;
+#pragma unroll
+      for (int q = 0; q < R; ++q) c[q] += id <= (uint32_t)w[q] ? y : 0.0;
+    }
+  uint32_t tok = 0xffffffffu, last = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (32 * r + lane < keep) {
+      last = max(last, (uint32_t)w[r]);
+      if (c[r] > u * z) tok = min(tok, (uint32_t)w[r]);
+    }
+  tok = __reduce_min_sync(0xffffffffu, tok);
+  last = __reduce_max_sync(0xffffffffu, last);
+  return (int)(tok != 0xffffffffu ? tok : last);
+}
+
 // ---- the kernel -----------------------------------------------------------------------------------------------------
 // Row r is block r; with CL, ranks [0, gridDim.x) of cluster r, each with `per_rank` stretches.
 template <typename T, bool CL>
-__global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(const Args p, const int per_rank) {
+__global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int per_rank) {
   pdl_trigger();
   __shared__ Scratch s;
   Group<CL> g{s, (int)threadIdx.x, (int)threadIdx.x & 31, (int)threadIdx.x >> 5, (int)blockDim.x >> 5, CL ? (int)blockIdx.x : 0, CL ? (int)gridDim.x : 1};
@@ -264,29 +368,41 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
   const bool wide = reinterpret_cast<uintptr_t>(lr) % (4 * sizeof(T)) == 0;
   pdl_wait();
 
-  // f(logit, id) for this thread's ids of stretch q
-  auto in_stretch = [&](int q, auto&& f) {
-    const int i0 = q * kStretch + 4 * g.lane;
-    float v[16];
-    if (wide && (q + 1) * kStretch <= p.V) {
+  // f(16 logits, stretch): this thread's of the block's stretches. Loops and bodies are kept short: most of this kernel's code runs
+  // once or twice per row, so that instructions are fetched anew, and bodies unrolled over the 16 cost more than they saved.
+  auto id_at = [&](int q, int j) { return q * kStretch + (wide ? 128 * (j >> 2) + 4 * g.lane + (j & 3) : 32 * j + g.lane); };
+  auto each16 = [&](auto&& f) {
+#pragma unroll 1
+    for (int q = q0 + g.warp; q < q1; q += g.warps) {
+      float v[16];
+      if (wide && (q + 1) * kStretch <= p.V) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 x = ld4(lr + i0 + 128 * j);
-        v[4 * j] = x.x; v[4 * j + 1] = x.y; v[4 * j + 2] = x.z; v[4 * j + 3] = x.w;
-      }
-    } else {
+        for (int j = 0; j < 4; ++j) {
+          const float4 x = ld4(lr + q * kStretch + 128 * j + 4 * g.lane);
+          v[4 * j] = x.x; v[4 * j + 1] = x.y; v[4 * j + 2] = x.z; v[4 * j + 3] = x.w;
+        }
+      } else {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int i = i0 + 128 * (j >> 2) + (j & 3);
-        v[j] = i < p.V ? to_float(lr[i]) : -INFINITY;
+        for (int j = 0; j < 16; ++j) {
+          const int i = id_at(q, j);
+          v[j] = i < p.V ? to_float(lr[i]) : -INFINITY;
+        }
       }
+      f(v, q);
     }
-#pragma unroll
-    for (int j = 0; j < 16; ++j) f(v[j], i0 + 128 * (j >> 2) + (j & 3));
   };
+  auto largest = [](const float (&v)[16]) {          // NaN if one of them is
+    float m = max3_nan(v[0], v[1], v[2]);
+#pragma unroll
+    for (int j = 3; j < 15; j += 2) m = max3_nan(m, v[j], v[j + 1]);
+    return max3_nan(m, v[15], v[15]);
+  };
+  // f(logit, id), one by one
   auto each = [&](auto&& f) {
 #pragma unroll 1
-    for (int q = q0 + g.warp; q < q1; q += g.warps) in_stretch(q, f);
+    for (int q = q0 + g.warp; q < q1; q += g.warps)
+#pragma unroll 4
+      for (int i = q * kStretch + g.lane; i < min(p.V, (q + 1) * kStretch); i += 32) f(to_float(lr[i]), i);
   };
 
   // ---- parameters and the maximum ----
@@ -296,12 +412,14 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
   const int top_k = k0 <= 0 || k0 > p.V ? p.V : k0;
   const double top_p = p0 < 1.0f ? (double)fmaxf(p0, 0.0f) : 1.0, min_p = f0 > 0.0f ? (double)fminf(f0, 1.0f) : 0.0, u = u0 > 0.0f ? (double)u0 : 0.0;
   float top = -INFINITY;                             // this thread's largest logit
-  bool odd = false;
-  each([&](float l, int) {
-    odd |= !(l < INFINITY);
-    top = fmaxf(top, l);                             // (a NaN masks its token: it fails every comparison)
-  });
-  if (odd) raise_status(p.status, kStatusNonFinite);
+  each16([&](const float (&v)[16], int) { top = max3_nan(top, largest(v), top); });
+  if (!(top < INFINITY)) {
+    raise_status(p.status, kStatusNonFinite);
+    if (top != top) {                                // a NaN masks its token: it fails every comparison
+      top = -INFINITY;
+      each([&](float l, int) { top = fmaxf(top, l); });
+    }
+  }
   const float l_max = g.max_of(top);
   if (l_max == -INFINITY) {                          // nothing can be picked
     if (g.tid == 0 && g.rank == 0) { raise_status(p.status, kStatusNonFinite); p.tok[row] = 0; }
@@ -316,13 +434,17 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
     if (CL) g.sync_all();
     return;
   }
-  const double rate64 = 1.4426950408889634074 / (double)T0;            // 1 / (T ln 2)
+  // T ln 2, and its reciprocal: the fp32 one and two Newton steps (a division would be forty instructions in every warp)
+  const double octave = (double)fminf(T0, 1e38f) * 0.693147180559945309417;
+  double rate64 = (double)(1.0f / (float)octave);
+  rate64 = fma(rate64, fma(-octave, rate64, 1.0), rate64);
+  rate64 = fma(rate64, fma(-octave, rate64, 1.0), rate64);
   const float rate = (float)fmin(rate64, 3e38);
   auto weight = [&](float l) { return l == l_max ? 1.0f : ex2(fmaxf(l - l_max, -3e38f) * rate); };
   auto weight_of = [&](float l) { return weight64(l, l_max, rate64); };
   // the logit with weight 2^x, as a finite float
   auto logit_at = [&](double x) {
-    const double v = (double)l_max + x / rate64;
+    const double v = fma(x, octave, (double)l_max);
     return v > -3.4e38 ? (float)v : -3.402823466e38f;
   };
   const bool limit_k = top_k < p.V, limit_p = top_p < 1.0;
@@ -330,12 +452,14 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
   // min_p as logits: surely below, surely above
   float floor_lo = least, floor_hi = least;
   if (min_p > 0.0 && l_max < INFINITY) {
-    const double v = (double)l_max + log2(min_p) / rate64, off = 1e-6 * (fabs(v) + fabs((double)l_max));
+    const double x = (double)__log2f((float)min_p), v = fma(x, octave, (double)l_max);       // (2^-22 off at most)
+    const double off = 1e-6 * (fabs(v) + fabs((double)l_max) + octave * (1.0 - x));
     floor_lo = fmaxf(least, v - off > -3.4e38 ? (float)(v - off) : least);
     floor_hi = fmaxf(least, v + off > -3.4e38 ? (float)(v + off) : least);
   }
 
   // ---- thresholds lo < hi: {l >= lo} holds all that is kept, {l >= hi} is kept (above min_p); counts and masses ----
+  const float no_top = __int_as_float(0x7fffffff);                     // (nothing compares as at or above a NaN)
   const float beyond = INFINITY;                     // hi: nothing lies above it (l_max of infinity is told apart by `whole`)
   float lo = least, hi = beyond, m_lo = 0.f, m_hi = 0.f, Z = 0.f;
   uint32_t n_lo = 0xffffffffu, n_hi = 0;
@@ -352,12 +476,17 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
     for (int i = 0; i < 3; ++i) { m3[i] = 0.f; n3[i] = 0u; x3[i] = 0.0; }
     float z = 0.f;
     if (!exact) {
-      each([&](float l, int) {
-        const float w = l >= least ? weight(l) : 0.f;
-        z += w;
+      const bool inf = l_max == INFINITY;
+      each16([&](const float (&v)[16], int) {
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-          if (l >= t3[i]) { m3[i] += w; ++n3[i]; }
+        for (int j = 0; j < 16; ++j) {
+          float w = ex2(fmaxf(v[j] - l_max, -3e38f) * rate);
+          if (inf) w = v[j] == l_max ? 1.0f : 0.0f;
+          z += w;
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+            if (v[j] >= t3[i]) { m3[i] += w; ++n3[i]; }
+        }
       });
     } else {
       each([&](float l, int) {
@@ -434,14 +563,24 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
   int n = 0;
   auto collect_begin = [&]() {
     if (g.tid == 0) s.count = 0;
-    g.sync_all();
+    __syncthreads();
   };
   auto collect = [&](float l, int id) {
-    const uint32_t at = atomicAdd(&lead.count, 1u);
-    if (at < (uint32_t)kCap) lead.cand[at] = word_of(l, id);
+    const uint32_t at = atomicAdd(&s.count, 1u);
+    if (at < (uint32_t)kCap) s.cand[at] = word_of(l, id);
   };
   auto collect_end = [&]() {
     g.sync_all();
+    if (CL) {                                        // the other ranks' behind the leading rank's own
+      if (g.rank != 0) {
+        const uint32_t mine = s.count;
+        if (g.tid == 0) s.n[0][0] = atomicAdd(&lead.count, mine);
+        __syncthreads();
+        const uint32_t base = s.n[0][0];
+        for (uint32_t i = g.tid; i < min(mine, (uint32_t)kCap) && base + i < (uint32_t)kCap; i += threads) lead.cand[base + i] = s.cand[i];
+      }
+      g.sync_all();
+    }
     n = (int)min(lead.count, (uint32_t)kCap + 1u);
     g.sync_all();
     return (uint32_t)n;
@@ -463,10 +602,24 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
     __syncthreads();
     running_sums(s.weight, s.run, n, g.tid, threads, s.d[0]);
   };
+  // This thread's tokens of a stretch in [from, to) to the list: as a mask first, so that all lanes add their first one at once (a
+  // branch per logit cost 5000 clocks a pass); the logit is read again.
+  auto pick = [&](const float (&v)[16], int q, float from, float to) {
+    uint32_t mask = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) mask |= v[j] >= from && !(v[j] >= to) ? 1u << j : 0u;
+#pragma unroll 1
+    while (mask != 0u) {
+      const int i = id_at(q, __ffs(mask) - 1);
+      mask &= mask - 1u;
+      collect(to_float(lr[i]), i);
+    }
+  };
   auto gather = [&]() {
     collect_begin();
-    each([&](float l, int id) {
-      if (l >= lo && (whole || l < hi)) collect(l, id);
+    const float from = lo, to = whole ? no_top : hi;
+    each16([&](const float (&v)[16], int q) {
+      if (!(largest(v) < from)) pick(v, q, from, to);
     });
     return collect_end();
   };
@@ -476,14 +629,16 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
 #pragma unroll 1
     for (int q = q0 + g.warp; q < q1; q += g.warps) {
       double in = 0.0;
-      in_stretch(q, [&](float l, int id) {
-        const bool k = l >= least && kept(l, id);
+#pragma unroll 4
+      for (int i = q * kStretch + g.lane; i < min(p.V, (q + 1) * kStretch); i += 32) {
+        const float l = to_float(lr[i]);
+        const bool k = l >= least && kept(l, i);
         if (k || (all && l >= least)) {
           const double w = weight_of(l);
           x += w;
           in += k ? w : 0.0;
         }
-      });
+      }
       in = warp_sum64(in);
       y += in;
       if (g.lane == 0) lead.part[q] = in;
@@ -527,13 +682,26 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
   double mass_k = -1.0;                              // mass of the first top_k, once known
   const int guess = limit_k ? top_k : 64;            // a threshold that about so many tokens reach
   float first = -INFINITY;
-  if ((limit_k || limit_p) && 2 * guess <= threads) {
+  const int goal = CL ? (guess + g.ranks - 1) / g.ranks : guess;        // of this block
+  if ((limit_k || limit_p) && 2 * goal <= threads) {
+    // the guess-th largest of the threads' maxima, halving keys until few more threads reach it
     const uint32_t key = logit_key(top);
-    uint32_t t = 0;
-    for (int b = 31; b >= 16; --b)                   // 16 bits of it
-      if (__syncthreads_count(key >= (t | (1u << b))) >= guess) t |= 1u << b;
-    first = t != 0u ? key_logit(t) : -INFINITY;
-    if (CL) first = g.max_of(first);                 // (the rank that has it alone has as many)
+    uint32_t a = ~g.block_max(key != 0u ? ~key : 0u), b = logit_key(l_max) + 1u;      // a: all that have one, b: too few
+    if (__syncthreads_count(key != 0u) >= goal) {
+#pragma unroll 1
+      for (int i = 0; i < 16 && b - a > 1u; ++i) {
+        const uint32_t t = a + (b - a) / 2;
+        const int c = __syncthreads_count(key >= t);
+        if (c >= goal) {
+          a = t;
+          if (c <= goal + goal / 8 + 2) break;
+        } else {
+          b = t;
+        }
+      }
+      first = key_logit(a);
+    }
+    if (CL) first = -g.max_of(-first);               // (every rank has its share of them above the least)
   }
   const float floor_list = limit_k && limit_p ? least : floor_lo;      // (top_p counts the mass of top_k without regard to min_p)
   if (limit_k) {
@@ -608,17 +776,26 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
       const bool try_list = first > -INFINITY;
       if (try_list) collect_begin();
       float z = 0.f, a0 = 0.f, a1 = 0.f, a2 = 0.f;
-      uint32_t c0 = 0, c1 = 0, c2 = 0;
-      each([&](float l, int id) {
-        const float w = l >= least ? weight(l) : 0.f;
-        z += w;
-        if (l >= t3[2]) { a2 += w; ++c2; }
-        if (l >= t3[1]) { a1 += w; ++c1; }
-        if (l >= t3[0]) { a0 += w; ++c0; if (try_list) collect(l, id); }
+      uint32_t c0 = 0, c1 = 0, c2 = 0, none = 0;
+      const bool inf = l_max == INFINITY;
+      const float ta = t3[0], tb = t3[1], tc = t3[2];
+      each16([&](const float (&v)[16], int q) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          // (a NaN or minus infinity ends as 0, the maximum as 1; weights under 2^-80 do no harm)
+          float w = ex2(fmaxf(v[i] - l_max, -3e38f) * rate);
+          if (inf) w = v[i] == l_max ? 1.0f : 0.0f;
+          z += w;
+          if (v[i] >= tc) { a2 += w; ++c2; }
+          if (v[i] >= tb) { a1 += w; ++c1; }
+          if (v[i] >= ta) { a0 += w; ++c0; }
+        }
+        if (try_list && !(largest(v) < ta)) pick(v, q, ta, no_top);
       });
-      uint32_t none = 0;
       g.add(z, none);
-      g.add(a0, c0); g.add(a1, c1); g.add(a2, c2);
+      g.add(a0, c0);
+      g.add(a1, c1);
+      g.add(a2, c2);
       Z = z;
       m3[0] = a0; m3[1] = a1; m3[2] = a2;
       n3[0] = c0; n3[1] = c1; n3[2] = c2;
@@ -674,6 +851,26 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
     whole = whole || listed;
     if (whole) n_hi = 0;
     if (!listed) gather();
+    if (whole && n <= 128) {
+      const bool of_list = by_k && mass_k < 0.0, rough = by_mass && mass_k < 0.0 && !by_k;
+      int tok = 0;
+      if (g.rank == 0 && g.warp == 0) {
+        const double total = mass_k >= 0.0 ? mass_k : of_list ? -1.0 : (double)Z, off = rough ? 2.0 * (double)kSlack * (double)Z : 0.0;
+        const int k_left = by_k ? top_k : n;
+        if (n <= 64) tok = short_list<2>(s.cand, n, k_left, by_mass, top_p, total, off, border, min_p, u, g.lane, weight_of);
+        else tok = short_list<4>(s.cand, n, k_left, by_mass, top_p, total, off, border, min_p, u, g.lane, weight_of);
+        if (g.lane == 0 && tok >= 0) p.tok[row] = tok;
+      }
+      if (rough) {                                   // the fp32 total may not be enough
+        double t = (double)tok, none = 0.0;
+        tell(t, none, t, none);
+        tok = (int)t;
+      }
+      if (!rough || tok >= 0) {
+        if (CL) g.sync_all();
+        return;
+      }
+    }
     order();
     const float above = hi;
     const bool sums = !whole;
@@ -715,7 +912,7 @@ __global__ void __launch_bounds__(CL ? 1024 : 512, CL ? 1 : 2) sample_kernel(con
 #pragma unroll 1
     for (int q = q0 + g.warp; q < q1; q += g.warps) {
       uint32_t c = 0;
-      in_stretch(q, [&](float l, int) { c += l == v ? 1u : 0u; });
+      for (int i = q * kStretch + g.lane; i < min(p.V, (q + 1) * kStretch); i += 32) c += to_float(lr[i]) == v ? 1u : 0u;
       c = __reduce_add_sync(0xffffffffu, c);
       if (g.lane == 0) lead.ties[q] = c;
     }
