@@ -192,7 +192,7 @@ int srm_k_quant_fp8(int64_t R, int64_t K, const void* d_x, int32_t x_dtype, int6
   if (R < 0 || K < 1 || !dtype_ok(x_dtype) || (block_rows != 1 && block_rows != 128)) return SRM_ERR_INVALID_ARG;
   const int64_t kb = (K + 127) / 128;
   if (K % 16 || kb > kMaxGrid || R > kMaxGrid) return SRM_ERR_UNSUPPORTED;
-  const int64_t grid = block_rows == 1 ? (R * kb + q8::kQuantThreads / 32 - 1) / (q8::kQuantThreads / 32) : (R + 127) / 128 * kb;
+  const int64_t grid = block_rows == 1 ? (R * kb + q8::kQuantThreads / 16 - 1) / (q8::kQuantThreads / 16) : (R + 127) / 128 * kb;
   if (grid > kMaxGrid) return SRM_ERR_UNSUPPORTED;
   if (R == 0) return SRM_OK;
   int rc;

@@ -104,8 +104,8 @@ struct Scratch {
   double d[2][kMaxWarps], rank_d[2][kMaxRanks];
   float f[2][kMaxWarps], rank_f[2][kMaxRanks];
   uint32_t n[2][kMaxWarps], rank_n[2][kMaxRanks];
-  float f3[3][kMaxWarps], rank_f3[3][kMaxRanks];
-  uint32_t n3[3][kMaxWarps], rank_n3[3][kMaxRanks];
+  float f4[2][4][kMaxWarps], rank_f4[2][kMaxRanks][4];
+  uint32_t n3[2][3][kMaxWarps], rank_n3[2][kMaxRanks][3];
   uint32_t count;
   int keep, unsure, tok, last;
   double box[2];                       // from the leading rank to the others
@@ -166,22 +166,44 @@ struct Group {
     }
     return v;
   }
-  // a sum of masses and one of counts
-  __device__ void add(float& m, uint32_t& n) {
+  // four masses and three counts at once
+  __device__ void add7(float (&m)[4], uint32_t (&n)[3]) {
     const int b = turn;
     turn ^= 1;
-    m = srm::warp_sum(m);
-    n = __reduce_add_sync(0xffffffffu, n);
-    if (lane == 0) { s.f[b][warp] = m; s.n[b][warp] = n; }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = srm::warp_sum(m[i]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) n[i] = __reduce_add_sync(0xffffffffu, n[i]);
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.f4[b][i][warp] = m[i];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) s.n3[b][i][warp] = n[i];
+    }
     __syncthreads();
-    m = srm::warp_sum(lane < warps ? s.f[b][lane] : 0.f);
-    n = __reduce_add_sync(0xffffffffu, lane < warps ? s.n[b][lane] : 0u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = srm::warp_sum(lane < warps ? s.f4[b][i][lane] : 0.f);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) n[i] = __reduce_add_sync(0xffffffffu, lane < warps ? s.n3[b][i][lane] : 0u);
     if (CL) {
-      if (tid == 0) { to_ranks(s.rank_f[b], m); to_ranks(s.rank_n[b], n); }
+      if (tid < ranks) {                             // a thread per rank
+        Scratch& to = *cooperative_groups::this_cluster().map_shared_rank(&s, tid);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to.rank_f4[b][rank][i] = m[i];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) to.rank_n3[b][rank][i] = n[i];
+      }
       sync_all();
-      m = 0.f;
-      n = 0u;
-      for (int r = 0; r < ranks; ++r) { m += s.rank_f[b][r]; n += s.rank_n[b][r]; }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        m[i] = 0.f;
+        for (int r = 0; r < ranks; ++r) m[i] += s.rank_f4[b][r][i];
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        n[i] = 0u;
+        for (int r = 0; r < ranks; ++r) n[i] += s.rank_n3[b][r][i];
+      }
     }
   }
   __device__ double add64(double m) {
@@ -332,7 +354,7 @@ __device__ __noinline__ int short_list(const unsigned long long* list, int n, in
   for (int r = 0; r < R; ++r) c[r] = 0.0;
 #pragma unroll
   for (int r = 0; r < R; ++r)
-#pragma unroll 2
+#pragma unroll 4
     for (int j = 0; j < min(32, keep - 32 * r); ++j) {
       const uint32_t id = __shfl_sync(0xffffffffu, (uint32_t)w[r], j);
       const double y = __shfl_sync(0xffffffffu, x[r], j);
@@ -468,48 +490,91 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   float m3[3];
   uint32_t n3[3];
   double x3[3];
+  // The list: collect_begin, the tokens of a range from all threads, collect_end (all ranks get their number).
+  int n = 0;
+  auto collect_begin = [&]() {
+    if (g.tid == 0) s.count = 0;
+    __syncthreads();
+  };
+  auto collect = [&](float l, int id) {
+    const uint32_t at = atomicAdd(&s.count, 1u);
+    if (at < (uint32_t)kCap) s.cand[at] = word_of(l, id);
+  };
+  auto collect_end = [&]() {
+    g.sync_all();
+    if (CL) {                                        // the other ranks' behind the leading rank's own
+      if (g.rank != 0) {
+        const uint32_t mine = s.count;
+        if (g.tid == 0) s.n[0][0] = atomicAdd(&lead.count, mine);
+        __syncthreads();
+        const uint32_t base = s.n[0][0];
+        for (uint32_t i = g.tid; i < min(mine, (uint32_t)kCap) && base + i < (uint32_t)kCap; i += threads) lead.cand[base + i] = s.cand[i];
+      }
+      g.sync_all();
+    }
+    n = (int)min(lead.count, (uint32_t)kCap + 1u);
+    g.sync_all();
+    return (uint32_t)n;
+  };
+  // This thread's tokens of a stretch in [from, to) to the list: as a mask first, so that all lanes add their first one at once (a
+  // branch per logit cost 5000 clocks a pass); the logit is read again.
+  auto pick = [&](const float (&v)[16], int q, float from, float to) {
+    uint32_t mask = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) mask |= v[j] >= from && !(v[j] >= to) ? 1u << j : 0u;
+#pragma unroll 1
+    while (mask != 0u) {
+      const int i = id_at(q, __ffs(mask) - 1);
+      mask &= mask - 1u;
+      collect(to_float(lr[i]), i);
+    }
+  };
   // Counts and masses at or above three thresholds t3[0] >= t3[1] >= t3[2], and the mass of everything.
   float t3[3];
-  auto sum3 = [&](bool exact) {
-    double all = 0.0;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) { m3[i] = 0.f; n3[i] = 0u; x3[i] = 0.0; }
-    float z = 0.f;
+  auto sum3 = [&](bool exact, bool list) {
     if (!exact) {
       const bool inf = l_max == INFINITY;
-      each16([&](const float (&v)[16], int) {
+      const float a = t3[0], b = t3[1], c = t3[2];
+      float m[4] = {0.f, 0.f, 0.f, 0.f};
+      uint32_t k[3] = {0u, 0u, 0u};
+      each16([&](const float (&v)[16], int q) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          float w = ex2(fmaxf(v[j] - l_max, -3e38f) * rate);
-          if (inf) w = v[j] == l_max ? 1.0f : 0.0f;
-          z += w;
-#pragma unroll
-          for (int i = 0; i < 3; ++i)
-            if (v[j] >= t3[i]) { m3[i] += w; ++n3[i]; }
+        for (int i = 0; i < 16; ++i) {
+          // (a NaN or minus infinity ends as 0, the maximum as 1; weights under 2^-80 do no harm)
+          float w = ex2(fmaxf(v[i] - l_max, -3e38f) * rate);
+          if (inf) w = v[i] == l_max ? 1.0f : 0.0f;
+          m[3] += w;
+          if (v[i] >= c) { m[2] += w; ++k[2]; }
+          if (v[i] >= b) { m[1] += w; ++k[1]; }
+          if (v[i] >= a) { m[0] += w; ++k[0]; }
         }
+        if (list && !(largest(v) < a)) pick(v, q, a, no_top);
       });
+      g.add7(m, k);
+      Z = m[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) { m3[i] = m[i]; n3[i] = k[i]; x3[i] = (double)m[i]; }
     } else {
+      double all = 0.0;
+      uint32_t k[3] = {0u, 0u, 0u};
+#pragma unroll
+      for (int i = 0; i < 3; ++i) x3[i] = 0.0;
       each([&](float l, int) {
         if (l >= least) {
           const double w = weight_of(l);
           all += w;
 #pragma unroll
           for (int i = 0; i < 3; ++i)
-            if (l >= t3[i]) { x3[i] += w; ++n3[i]; }
+            if (l >= t3[i]) { x3[i] += w; ++k[i]; }
         }
       });
       all64 = g.add64(all);
 #pragma unroll
       for (int i = 0; i < 3; ++i) x3[i] = g.add64(x3[i]);
-    }
+      float unused[4] = {0.f, 0.f, 0.f, 0.f};
+      g.add7(unused, k);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) g.add(m3[i], n3[i]);
-    uint32_t none = 0;
-    if (!exact) {
-      g.add(z, none);
-      Z = z;
-#pragma unroll
-      for (int i = 0; i < 3; ++i) x3[i] = (double)m3[i];
+      for (int i = 0; i < 3; ++i) n3[i] = k[i];
     }
   };
   // Takes over what a threshold says. by_count: the border is token want_n of the order; else where the mass reaches want.
@@ -551,7 +616,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       }
       const bool quarters = !unbounded && !((it & 1) && hi < beyond);
       const float lo_was = lo, hi_was = hi;
-      sum3(exact);
+      sum3(exact, false);
       place(by_count, want_n, want, slack, exact ? all64 : (double)Z);
       if (unbounded && n_lo == 0xffffffffu && t3[2] <= least) { lo = least; n_lo = n3[2]; m_lo = (float)x3[2]; }
       if (!exact && !by_count && quarters && lo == lo_was && hi == hi_was) break;
@@ -559,33 +624,8 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
     whole = false;
     return n_lo != 0xffffffffu && n_lo - n_hi <= (uint32_t)kCap;
   };
-  // The tokens of [lo, hi) as sorted words with weights and running sums, in the leading rank; all ranks get their number.
-  int n = 0;
-  auto collect_begin = [&]() {
-    if (g.tid == 0) s.count = 0;
-    __syncthreads();
-  };
-  auto collect = [&](float l, int id) {
-    const uint32_t at = atomicAdd(&s.count, 1u);
-    if (at < (uint32_t)kCap) s.cand[at] = word_of(l, id);
-  };
-  auto collect_end = [&]() {
-    g.sync_all();
-    if (CL) {                                        // the other ranks' behind the leading rank's own
-      if (g.rank != 0) {
-        const uint32_t mine = s.count;
-        if (g.tid == 0) s.n[0][0] = atomicAdd(&lead.count, mine);
-        __syncthreads();
-        const uint32_t base = s.n[0][0];
-        for (uint32_t i = g.tid; i < min(mine, (uint32_t)kCap) && base + i < (uint32_t)kCap; i += threads) lead.cand[base + i] = s.cand[i];
-      }
-      g.sync_all();
-    }
-    n = (int)min(lead.count, (uint32_t)kCap + 1u);
-    g.sync_all();
-    return (uint32_t)n;
-  };
-  auto order = [&]() {                               // (after collect_end, at most kCap)
+  // The list sorted, with weights and running sums (leading rank).
+  auto order = [&]() {
     if (g.rank != 0) return;
     unsigned long long* other = reinterpret_cast<unsigned long long*>(s.run);
     if (n <= 192) {
@@ -601,19 +641,6 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
     }
     __syncthreads();
     running_sums(s.weight, s.run, n, g.tid, threads, s.d[0]);
-  };
-  // This thread's tokens of a stretch in [from, to) to the list: as a mask first, so that all lanes add their first one at once (a
-  // branch per logit cost 5000 clocks a pass); the logit is read again.
-  auto pick = [&](const float (&v)[16], int q, float from, float to) {
-    uint32_t mask = 0;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) mask |= v[j] >= from && !(v[j] >= to) ? 1u << j : 0u;
-#pragma unroll 1
-    while (mask != 0u) {
-      const int i = id_at(q, __ffs(mask) - 1);
-      mask &= mask - 1u;
-      collect(to_float(lr[i]), i);
-    }
   };
   auto gather = [&]() {
     collect_begin();
@@ -712,7 +739,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       if (!listed) {                                 // (more than the list counted)
         if (lo > floor_list) {
           t3[0] = t3[1] = t3[2] = lo;
-          sum3(false);
+          sum3(false, false);
           n_lo = n3[0];
           m_lo = m3[0];
         } else {
@@ -726,7 +753,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       listed = n_lo <= (uint32_t)kCap;
       if (!listed) {
         t3[0] = t3[1] = t3[2] = lo;
-        sum3(false);
+        sum3(false, false);
         n_lo = n3[0];
         by_k = n_lo >= (uint32_t)top_k;
         if (by_k) n_lo = 0xffffffffu;                // (the search begins at the top)
@@ -775,32 +802,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       if (t3[2] > t3[1]) t3[2] = t3[1];
       const bool try_list = first > -INFINITY;
       if (try_list) collect_begin();
-      float z = 0.f, a0 = 0.f, a1 = 0.f, a2 = 0.f;
-      uint32_t c0 = 0, c1 = 0, c2 = 0, none = 0;
-      const bool inf = l_max == INFINITY;
-      const float ta = t3[0], tb = t3[1], tc = t3[2];
-      each16([&](const float (&v)[16], int q) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          // (a NaN or minus infinity ends as 0, the maximum as 1; weights under 2^-80 do no harm)
-          float w = ex2(fmaxf(v[i] - l_max, -3e38f) * rate);
-          if (inf) w = v[i] == l_max ? 1.0f : 0.0f;
-          z += w;
-          if (v[i] >= tc) { a2 += w; ++c2; }
-          if (v[i] >= tb) { a1 += w; ++c1; }
-          if (v[i] >= ta) { a0 += w; ++c0; }
-        }
-        if (try_list && !(largest(v) < ta)) pick(v, q, ta, no_top);
-      });
-      g.add(z, none);
-      g.add(a0, c0);
-      g.add(a1, c1);
-      g.add(a2, c2);
-      Z = z;
-      m3[0] = a0; m3[1] = a1; m3[2] = a2;
-      n3[0] = c0; n3[1] = c1; n3[2] = c2;
-#pragma unroll
-      for (int i = 0; i < 3; ++i) x3[i] = (double)m3[i];
+      sum3(false, try_list);
       want = top_p * (double)Z;
       place(false, 0, want, (double)kSlack, (double)Z);
       // the first list serves if the nucleus, or min_p, ends inside it
