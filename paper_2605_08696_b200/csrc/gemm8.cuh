@@ -226,18 +226,26 @@ __global__ void __launch_bounds__(Few<NT>::kThreads) gemm8_few_kernel(const __gr
 // ones they add: they take the registers that the warpgroup of the loads and the MMAs gives up. A warp of its own keeps the
 // scales of the next blocks coming into shared memory (fetched by the adding warps one block ahead they cost 330 of 1220 clocks a
 // block). What bounds it now is the adding: 256 of a block's 512 clocks are the fused multiply-adds alone.
+// A tile's output is staged whole (64 KB per CTA in bf16, 128 KB in fp32, which leaves three stages for the operands), and stored while
+// the next tile is computed: all CTAs finish their tiles at about the same time, so that the stores come in bursts that memory takes
+// as long for as the tile's products (with half of an fp32 tile staged, the adding warps waited for the other half: M = 4096,
+// N = 32000, K = 1024: 212 us).
+template <typename OT>
 struct Many {
-  static constexpr int kStages = 4;
-  static constexpr int kSlots = 8;                                      // blocks whose scales are there: the stages, two accumulators, one
+  static constexpr int kCols = 128;
+  static constexpr int kBoxes = kCols * (int)sizeof(OT) / 128;          // of a warp
+  static constexpr int kStages = sizeof(OT) == 4 ? 3 : 4;
+  static constexpr int kSlots = kStages + 2;                            // blocks whose scales are there: the stages, two accumulators
   static constexpr int kABytes = 128 * kBK, kWBytes = 128 * kBK;       // per CTA and block
   static constexpr int kStage = kABytes + kWBytes;
   static constexpr int kAddWarps = 8;
-  static constexpr int kCols = 128;
   static constexpr int kThreads = 128 + 32 * kAddWarps;                 // 168 registers a thread at launch
   static constexpr int kRegsFew = 40, kRegsAdd = 232;                   // 4 x 40 + 8 x 232 = 12 x 168 (warps)
-  static constexpr int kBox = 32 * 128;                                 // staged output: 32 rows x 128 bytes, two per warp
+  static constexpr int kBox = 32 * 128;                                 // staged output: 32 rows x 128 bytes
   static constexpr int kScales = kSlots * 130 * 4;                      // per slot: 128 rows, 2 groups of 128 columns
-  static constexpr int kBytes = kStages * kStage + kAddWarps * 2 * kBox + kScales + 256 + 1024;
+  static constexpr int kBarriers = (2 * kStages + 4 + kSlots + 1) * 8;
+  static constexpr int kBytes = kStages * kStage + kAddWarps * kBoxes * kBox + kScales + kBarriers;
+  static_assert(kBytes <= 232448, "shared memory of a block");
 };
 
 // A warp's staging box: 32 rows x 128 bytes of finished output (v: the lane's row), the 16-byte pieces of a row swizzled as the
@@ -268,21 +276,25 @@ __device__ __forceinline__ void write_box(const Args& g, const uint8_t* box, int
 // MAPPED: the output has a tensor map; BIAS: there is one. (Each its own kernel: with both in one, the code of a tile's output,
 // unrolled over 128 columns, missed the instruction cache every time and cost as much as six blocks of K.)
 template <typename OT, bool MAPPED, bool BIAS>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Many::kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(Many<OT>::kThreads, 1)
 gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmD,
                   const Args g) {
-  using F = Many;
+  using F = Many<OT>;
   pdl_trigger();
-  extern __shared__ uint8_t raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  // (no room for rounding up: a block's dynamic shared memory starts on a boundary of 1024 bytes where it has no static one)
+  extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* boxes = smem + F::kStages * F::kStage;
-  float* scales = reinterpret_cast<float*>(boxes + F::kAddWarps * 2 * F::kBox);
-  uint64_t* full = reinterpret_cast<uint64_t*>(boxes + F::kAddWarps * 2 * F::kBox + F::kScales);  // leader's: both CTAs' copies of a stage
+  float* scales = reinterpret_cast<float*>(boxes + F::kAddWarps * F::kBoxes * F::kBox);
+  uint64_t* full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(scales) + F::kScales);      // leader's: both CTAs' copies of a stage
   uint64_t* empty = full + F::kStages;                                  // per CTA: the stage may be filled again
   uint64_t* tfull = empty + F::kStages;                                 // per CTA [2]: a block's product is there
   uint64_t* tempty = tfull + 2;                                         // leader's [2]: both CTAs' warps have fetched it
   uint64_t* sfull = tempty + 2;                                         // per CTA [kSlots]: a block's scales are there
   uint32_t* slot = reinterpret_cast<uint32_t*>(sfull + F::kSlots);
+  if ((smem_addr(smem) & 1023u) != 0u) {                                // (never seen; every CTA alike)
+    raise_status(g.status, kStatusWaitTimeout);
+    return;
+  }
 
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cta_rank();
@@ -344,19 +356,19 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       }
     }
   } else if (warp == 2) {
-    // The scales of a block take the slot of the block eight before it, whose sums are done: this block's stage is free, so the
-    // MMAs are past the block four before it, and they are never more than two ahead of the sums.
-    int stage = 0;
-    uint32_t phase = 0, it = 0;
+    // A block's scales take the slot of the block kStages + 2 before it, whose sums are done: this block's stage is free, so the MMAs
+    // are past the block kStages before it, and they are never more than two blocks ahead of the sums.
+    int stage = 0, at = 0;
+    uint32_t phase = 0;
     bool ok = true;
     for (uint32_t q = first; ok && q < tiles; q += step) {
       const float* sa[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) sa[j] = g.sa + min((int64_t)(q % m_tiles * 256 + rank * 128 + j * 32 + lane), g.M - 1) * g.sa_row;
       const float* sw = g.sw + (min((int64_t)(q / m_tiles) * 256 + (lane & 1) * 128, g.N - 1) >> 7) * g.sw_row;
-      for (int kb = 0; kb < kbs; ++kb, ++it) {
+      for (int kb = 0; kb < kbs; ++kb) {
         if (!bar_wait(&empty[stage], phase ^ 1u, g.status)) { ok = false; break; }
-        float* to = scales + (it % F::kSlots) * 130;
+        float* to = scales + at * 130;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           copy4(smem_addr(to + j * 32 + lane), sa[j]);
@@ -364,7 +376,8 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         }
         if (lane < 2) copy4(smem_addr(to + 128 + lane), sw);
         sw += g.sw_blk;
-        copies_arrive(&sfull[it % F::kSlots]);
+        copies_arrive(&sfull[at]);
+        if (++at == F::kSlots) at = 0;
         if (++stage == F::kStages) { stage = 0; phase ^= 1u; }
       }
     }
@@ -372,99 +385,118 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   } else if (warp >= 4) {
     take_registers<F::kRegsAdd>();
     const int quad = warp & 3, cg = (warp - 4) >> 2;
-    uint8_t* box = boxes + (warp - 4) * 2 * F::kBox;
+    uint8_t* box = boxes + (warp - 4) * F::kBoxes * F::kBox;
     const uint32_t drained = peer_addr(smem_addr(&tempty[0]), 0);
     const uint32_t lanes = tm + ((uint32_t)(quad * 32) << 16) + cg * F::kCols;
-    uint32_t it = 0;
+    uint32_t it = 0, at = 0, at_phase = 0;
     bool ok = true;
     if (MAPPED && lane == 0) map_prefetch(&tmD);
+    constexpr int kPer = 128 / (int)sizeof(OT);                         // columns of a box
+    // The boxes of the last tile go out one by one, a block of K apart: the TMA unit takes its work in order, and the operands of the
+    // next blocks would wait behind a whole tile's stores (128 KB of fp32 took 3200 clocks of a tile's 12 400).
+    int64_t out_row = 0, out_col = 0;
+    int out_box = F::kBoxes;                                            // the next one to store
+    auto store_box = [&]() {
+      if (!MAPPED || out_box >= F::kBoxes) return;
+      const int64_t col = out_col + out_box * kPer;
+      if (col < g.N && one_lane()) {
+        const uint32_t src = smem_addr(box + out_box * F::kBox);
+        if (sizeof(OT) == 4 && g.accumulate) tile_add(&tmD, src, (int)col, (int)out_row);
+        else if (sizeof(OT) == 4) tile_store_streaming(&tmD, src, (int)col, (int)out_row);
+        else tile_store(&tmD, src, (int)col, (int)out_row);
+        stores_commit();
+      }
+      __syncwarp();
+      ++out_box;
+    };
     for (uint32_t q = first; ok && q < tiles; q += step) {
       const int64_t row0 = q % m_tiles * 256 + rank * 128 + quad * 32, col0 = (int64_t)(q / m_tiles) * 256 + cg * F::kCols;
-      float acc[F::kCols];
-      // one block: its scales, its product; the first one sets the sums
-      auto block = [&](auto set) {
-        const uint32_t buf = it & 1u, at = it % F::kSlots;
-        if (!bar_wait(&sfull[at], (it / F::kSlots) & 1u, g.status)) return false;
-        const float s = scales[at * 130 + quad * 32 + lane] * scales[at * 130 + 128 + cg];
-        if (!bar_wait(&tfull[buf], (it >> 1) & 1u, g.status)) return false;
+      float acc[F::kCols], s_next = 0.f;
+      uint32_t ra[32], rb[32];
+      // the next block: its scales, and the first columns of its product on their way
+      auto begin = [&]() {
+        if (!bar_wait(&sfull[at], at_phase, g.status)) return false;
+        s_next = scales[at * 130 + quad * 32 + lane] * scales[at * 130 + 128 + cg];
+        if (++at == (uint32_t)F::kSlots) { at = 0; at_phase ^= 1u; }
+        if (!bar_wait(&tfull[it & 1u], (it >> 1) & 1u, g.status)) return false;
         fence_after();
-        const uint32_t t = lanes + buf * 256;
-        uint32_t ra[32], rb[32];
-        tm_load32(t, ra);
-        tm_load_wait();
+        tm_load32(lanes + (it & 1u) * 256, ra);
+        return true;
+      };
+      // a block added (the first one sets the sums); the next one is begun before the last columns are
+      auto block = [&](auto set, bool more) {
+        const float s = s_next;
+        const uint32_t buf = it & 1u, t = lanes + buf * 256;
+        bool fine = true;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t (&cur)[32] = (c & 1) ? rb : ra;
           uint32_t (&nxt)[32] = (c & 1) ? ra : rb;
+          tm_load_wait();
           keep_order(cur);
-          if (c < 3) tm_load32(t + 32 * (c + 1), nxt);
+          if (c < 3) {
+            tm_load32(t + 32 * (c + 1), nxt);
+          } else {                                                      // everything has left tensor memory
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(drained + buf * 8u);
+            ++it;
+            if (more) fine = begin();
+          }
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             if (set) acc[32 * c + j] = s * __uint_as_float(cur[j]);
             else acc[32 * c + j] = fmaf(s, __uint_as_float(cur[j]), acc[32 * c + j]);
           }
-          if (c < 3) tm_load_wait();
-          if (c == 2) {                                                 // everything has left tensor memory
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(drained + buf * 8u);
-          }
         }
-        ++it;
-        return true;
+        return fine;
       };
-      ok = block(Yes());
-      for (int kb = 1; ok && kb < kbs; ++kb) ok = block(No());
+      ok = begin();
+      if (ok) ok = block(Yes(), kbs > 1);
+      store_box();
+      for (int kb = 1; ok && kb < kbs; ++kb) {
+        ok = block(No(), kb + 1 < kbs);
+        store_box();
+      }
       if (!ok) break;
+      while (MAPPED && out_box < F::kBoxes) store_box();
       if (row0 < g.M && col0 < g.N) {
-        constexpr int kPer = 128 / (int)sizeof(OT);                     // columns of a box
+        if (MAPPED && one_lane()) stores_wait_read();                   // the last tile's boxes have been read
+        __syncwarp();
 #pragma unroll
-        for (int c0 = 0; c0 < F::kCols; c0 += 2 * kPer) {
-          if (MAPPED && one_lane()) stores_wait_read();                 // the boxes have been read
-          __syncwarp();
+        for (int c = 0; c < F::kCols; c += kPer) {
+          uint32_t v[32];
 #pragma unroll
-          for (int c = c0; c < c0 + 2 * kPer; c += kPer) {
-            uint32_t v[32];
-#pragma unroll
-            for (int j = 0; j < kPer; j += 2) {
-              float x = acc[c + j], y = acc[c + j + 1];
-              if (BIAS) {
-                x += col0 + c + j < g.N ? __ldg(g.bias + col0 + c + j) : 0.f;
-                y += col0 + c + j + 1 < g.N ? __ldg(g.bias + col0 + c + j + 1) : 0.f;
-              }
-              if (sizeof(OT) == 4) {
-                v[j % 32] = __float_as_uint(x);
-                v[j % 32 + 1] = __float_as_uint(y);
-              } else {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
-                v[j / 2 % 32] = *reinterpret_cast<const uint32_t*>(&b);
-              }
+          for (int j = 0; j < kPer; j += 2) {
+            float x = acc[c + j], y = acc[c + j + 1];
+            if (BIAS) {
+              x += col0 + c + j < g.N ? __ldg(g.bias + col0 + c + j) : 0.f;
+              y += col0 + c + j + 1 < g.N ? __ldg(g.bias + col0 + c + j + 1) : 0.f;
             }
-            fill_box(box + (c / kPer & 1) * F::kBox, lane, v);
-          }
-          if (MAPPED) fence_async();
-          __syncwarp();
-          if (MAPPED) {
-            if (one_lane()) {
-#pragma unroll
-              for (int b = 0; b < 2; ++b) {
-                const int64_t col = col0 + c0 + b * kPer;
-                const uint32_t src = smem_addr(box + b * F::kBox);
-                if (col < g.N) {
-                  if (sizeof(OT) == 4 && g.accumulate) tile_add(&tmD, src, (int)col, (int)row0);
-                  else if (sizeof(OT) == 4) tile_store_streaming(&tmD, src, (int)col, (int)row0);
-                  else tile_store(&tmD, src, (int)col, (int)row0);
-                }
-              }
-              stores_commit();
+            if (sizeof(OT) == 4) {
+              v[j % 32] = __float_as_uint(x);
+              v[j % 32 + 1] = __float_as_uint(y);
+            } else {
+              const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+              v[j / 2 % 32] = *reinterpret_cast<const uint32_t*>(&b);
             }
-          } else {
-            write_box<OT>(g, box, lane, row0, col0 + c0);
-            write_box<OT>(g, box + F::kBox, lane, row0, col0 + c0 + kPer);
           }
+          fill_box(box + c / kPer * F::kBox, lane, v);
+        }
+        if (MAPPED) fence_async();
+        __syncwarp();
+        if (MAPPED) {
+          out_row = row0;
+          out_col = col0;
+          out_box = 0;
+        } else {
+#pragma unroll 1
+          for (int b = 0; b < F::kBoxes; ++b) write_box<OT>(g, box + b * F::kBox, lane, row0, col0 + b * kPer);
+          __syncwarp();
         }
       }
     }
+    while (MAPPED && out_box < F::kBoxes) store_box();
     if (MAPPED && one_lane()) stores_wait();                            // the boxes are out before shared memory goes away
   }
   fence_before();

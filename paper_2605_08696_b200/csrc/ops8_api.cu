@@ -96,7 +96,7 @@ int launch_many(const g8::Args& g, const uint8_t* A, int64_t a_stride, const uin
   const bool mapped = aligned(g.out, 16) && pitch * elem % 16 == 0;
   const auto kernel = mapped ? (g.bias != nullptr ? g8::gemm8_many_kernel<OT, true, true> : g8::gemm8_many_kernel<OT, true, false>)
                              : (g.bias != nullptr ? g8::gemm8_many_kernel<OT, false, true> : g8::gemm8_many_kernel<OT, false, false>);
-  int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), g8::Many::kBytes);
+  int rc = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), g8::Many<OT>::kBytes);
   if (rc != SRM_OK) return rc;
   CUtensorMap ta, tw, td;
   if ((rc = byte_map(&ta, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, g.M, g.K, map_stride(g.M, g.K, a_stride, 1), 128)) != SRM_OK) return rc;
@@ -106,7 +106,7 @@ int launch_many(const g8::Args& g, const uint8_t* A, int64_t a_stride, const uin
     return rc;
   const int64_t tiles = (g.M + 255) / 256 * ((g.N + 255) / 256), pairs = sms / 2;
   ++g_kernel_launches;
-  SRM_CUDA(launch_kernel(kernel, dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(g8::Many::kThreads), g8::Many::kBytes, st, ta, tw, td, g));
+  SRM_CUDA(launch_kernel(kernel, dim3(2u * (unsigned)(tiles < pairs ? tiles : pairs)), dim3(g8::Many<OT>::kThreads), g8::Many<OT>::kBytes, st, ta, tw, td, g));
   return SRM_OK;
 }
 
