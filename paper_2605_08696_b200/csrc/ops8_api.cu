@@ -136,13 +136,14 @@ int launch_sample(const smp::Args& p, cudaStream_t st) {
   int sms = 0;
   const int rc = device_sm_count(&sms);
   if (rc != SRM_OK) return rc;
-  const int stretches = (p.V + smp::kStretch - 1) / smp::kStretch;
+  const int ids = p.V <= smp::kFewIds ? 128 : 512, stretches = (p.V + ids - 1) / ids;
   ++g_kernel_launches;
   int ranks = 1;
-  while (ranks < smp::kMaxRanks && stretches > 32 * ranks && 2 * ranks * p.R <= sms) ranks *= 2;
+  while (ids == 512 && ranks < smp::kMaxRanks && stretches > 32 * ranks && 2 * ranks * p.R <= 2 * sms) ranks *= 2;
   if (ranks == 1) {
     const int warps = stretches < 16 ? stretches : 16;
-    SRM_CUDA(launch_kernel(smp::sample_kernel<T, false>, dim3((unsigned)p.R), dim3(32 * warps), 0, st, p, stretches));
+    SRM_CUDA(launch_kernel(ids == 128 ? smp::sample_kernel<T, false, 4> : smp::sample_kernel<T, false, 16>, dim3((unsigned)p.R), dim3(32 * warps), 0, st,
+                           p, stretches));
     return SRM_OK;
   }
   const int per_rank = (stretches + ranks - 1) / ranks, warps = per_rank < 16 ? per_rank : 16;
@@ -157,7 +158,7 @@ int launch_sample(const smp::Args& p, cudaStream_t st) {
   attr[1].val.clusterDim.x = (unsigned)ranks; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  SRM_CUDA(cudaLaunchKernelEx(&cfg, smp::sample_kernel<T, true>, p, per_rank));
+  SRM_CUDA(cudaLaunchKernelEx(&cfg, smp::sample_kernel<T, true, 16>, p, per_rank));
   return SRM_OK;
 }
 

@@ -48,7 +48,9 @@ template <typename T> __device__ __forceinline__ float load_logit(const Args& p,
   return to_float(static_cast<const T*>(p.logits)[row * p.stride + i]);
 }
 
-constexpr int kStretch = 512;                    // consecutive ids that a warp reads at a time: four groups of 128, four per lane
+// A warp reads `E` logits per lane at a time, a stretch of 32 E consecutive ids: 16, or 4 where the ids are few (more threads then share
+// a row, and their maxima tell more of it: 7380 rows of 1352 took 394 us with 16, for most of them sorted whole).
+constexpr int kFewIds = 8192;
 constexpr int kMaxStretches = 512;               // 262144 ids
 constexpr int kMaxWarps = 32;
 constexpr int kCap = 1024;                       // tokens that are sorted
@@ -376,8 +378,9 @@ __device__ __noinline__ int short_list(const unsigned long long* list, int n, in
 
 // ---- the kernel -----------------------------------------------------------------------------------------------------
 // Row r is block r; with CL, ranks [0, gridDim.x) of cluster r, each with `per_rank` stretches.
-template <typename T, bool CL>
+template <typename T, bool CL, int E>
 __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int per_rank) {
+  constexpr int kStretch = 32 * E;
   pdl_trigger();
   __shared__ Scratch s;
   Group<CL> g{s, (int)threadIdx.x, (int)threadIdx.x & 31, (int)threadIdx.x >> 5, (int)blockDim.x >> 5, CL ? (int)blockIdx.x : 0, CL ? (int)gridDim.x : 1};
@@ -396,16 +399,16 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   auto each16 = [&](auto&& f) {
 #pragma unroll 1
     for (int q = q0 + g.warp; q < q1; q += g.warps) {
-      float v[16];
+      float v[E];
       if (wide && (q + 1) * kStretch <= p.V) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < E / 4; ++j) {
           const float4 x = ld4(lr + q * kStretch + 128 * j + 4 * g.lane);
           v[4 * j] = x.x; v[4 * j + 1] = x.y; v[4 * j + 2] = x.z; v[4 * j + 3] = x.w;
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
+        for (int j = 0; j < E; ++j) {
           const int i = id_at(q, j);
           v[j] = i < p.V ? to_float(lr[i]) : -INFINITY;
         }
@@ -413,11 +416,11 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       f(v, q);
     }
   };
-  auto largest = [](const float (&v)[16]) {          // NaN if one of them is
+  auto largest = [](const float (&v)[E]) {          // NaN if one of them is
     float m = max3_nan(v[0], v[1], v[2]);
 #pragma unroll
-    for (int j = 3; j < 15; j += 2) m = max3_nan(m, v[j], v[j + 1]);
-    return max3_nan(m, v[15], v[15]);
+    for (int j = 3; j + 1 < E; j += 2) m = max3_nan(m, v[j], v[j + 1]);
+    return max3_nan(m, v[E - 1], v[E - 1]);
   };
   // f(logit, id), one by one
   auto each = [&](auto&& f) {
@@ -434,7 +437,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   const int top_k = k0 <= 0 || k0 > p.V ? p.V : k0;
   const double top_p = p0 < 1.0f ? (double)fmaxf(p0, 0.0f) : 1.0, min_p = f0 > 0.0f ? (double)fminf(f0, 1.0f) : 0.0, u = u0 > 0.0f ? (double)u0 : 0.0;
   float top = -INFINITY;                             // this thread's largest logit
-  each16([&](const float (&v)[16], int) { top = max3_nan(top, largest(v), top); });
+  each16([&](const float (&v)[E], int) { top = max3_nan(top, largest(v), top); });
   if (!(top < INFINITY)) {
     raise_status(p.status, kStatusNonFinite);
     if (top != top) {                                // a NaN masks its token: it fails every comparison
@@ -518,10 +521,10 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   };
   // This thread's tokens of a stretch in [from, to) to the list: as a mask first, so that all lanes add their first one at once (a
   // branch per logit cost 5000 clocks a pass); the logit is read again.
-  auto pick = [&](const float (&v)[16], int q, float from, float to) {
+  auto pick = [&](const float (&v)[E], int q, float from, float to) {
     uint32_t mask = 0;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) mask |= v[j] >= from && !(v[j] >= to) ? 1u << j : 0u;
+    for (int j = 0; j < E; ++j) mask |= v[j] >= from && !(v[j] >= to) ? 1u << j : 0u;
 #pragma unroll 1
     while (mask != 0u) {
       const int i = id_at(q, __ffs(mask) - 1);
@@ -537,9 +540,9 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       const float a = t3[0], b = t3[1], c = t3[2];
       float m[4] = {0.f, 0.f, 0.f, 0.f};
       uint32_t k[3] = {0u, 0u, 0u};
-      each16([&](const float (&v)[16], int q) {
+      each16([&](const float (&v)[E], int q) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < E; ++i) {
           // (a NaN or minus infinity ends as 0, the maximum as 1; weights under 2^-80 do no harm)
           float w = ex2(fmaxf(v[i] - l_max, -3e38f) * rate);
           if (inf) w = v[i] == l_max ? 1.0f : 0.0f;
@@ -645,7 +648,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   auto gather = [&]() {
     collect_begin();
     const float from = lo, to = whole ? no_top : hi;
-    each16([&](const float (&v)[16], int q) {
+    each16([&](const float (&v)[E], int q) {
       if (!(largest(v) < from)) pick(v, q, from, to);
     });
     return collect_end();
