@@ -581,6 +581,8 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
     }
   };
   // Takes over what a threshold says. by_count: the border is token want_n of the order; else where the mass reaches want.
+  bool even = false;                                 // a threshold, at `even_at`, with just the mass that is wanted (to the bounds)
+  float even_at = 0.f;
   auto place = [&](bool by_count, uint32_t want_n, double want, double slack, double total) {
 #pragma unroll
     for (int i = 2; i >= 0; --i) {
@@ -588,6 +590,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       const bool few = by_count ? n3[i] < want_n : x3[i] < want - (want + total) * slack;
       if (enough && t3[i] >= lo) { lo = t3[i]; n_lo = n3[i]; m_lo = (float)x3[i]; }
       if (few && t3[i] < hi) { hi = t3[i]; n_hi = n3[i]; m_hi = (float)x3[i]; }
+      if (!enough && !few) { even = true; even_at = t3[i]; }
     }
   };
   // Closes in until the first kCap of the order reach the border (whole), or at most kCap tokens lie between lo and hi. False: the
@@ -595,6 +598,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   auto search = [&](bool by_count, uint32_t want_n, double want, bool exact) {
     const double slack = exact ? kSlack64 : (double)kSlack;
     double down = 4.0;                               // octaves below the maximum, while nothing is known below
+    even = false;
     for (int it = 0; it < kRounds; ++it) {
       if (n_lo <= (uint32_t)kCap) { whole = true; return true; }
       if (n_lo != 0xffffffffu && n_lo - n_hi <= (uint32_t)kCap && (n_hi > (uint32_t)kCap / 2 || it > 4)) { whole = false; return true; }
@@ -621,11 +625,12 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       const float lo_was = lo, hi_was = hi;
       sum3(exact, false);
       place(by_count, want_n, want, slack, exact ? all64 : (double)Z);
+      if (exact && even) break;                      // the nucleus ends with the tokens that reach this threshold
       if (unbounded && n_lo == 0xffffffffu && t3[2] <= least) { lo = least; n_lo = n3[2]; m_lo = (float)x3[2]; }
       if (!exact && !by_count && quarters && lo == lo_was && hi == hi_was) break;
     }
     whole = false;
-    return n_lo != 0xffffffffu && n_lo - n_hi <= (uint32_t)kCap;
+    return !(exact && even) && n_lo != 0xffffffffu && n_lo - n_hi <= (uint32_t)kCap;
   };
   // The list sorted, with weights and running sums (leading rank).
   auto order = [&]() {
@@ -686,7 +691,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       const double b = before + (i > 0 ? s.run[i - 1] : 0.0);
       const bool in = i < k_left && s.cand[i] <= limit && (!by_floor || s.weight[i] >= min_p), first = i == 0 && before == 0.0;
       mine += in && (!by_mass || first || b < want) ? 1 : 0;
-      doubt |= by_mass && in && !first && fabs(b - want) <= off ? 1 : 0;
+      doubt |= by_mass && in && !first && fabs(b - want) < off ? 1 : 0;
     }
     if (mine) atomicAdd(&s.keep, mine);
     if (doubt) atomicOr(&s.unsure, 1);
@@ -828,7 +833,12 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
           want = top_p * all64;
         }
         ok = search(false, 0, want, true);
-        tie = !ok;
+        if (!ok && even) {                           // (a whole sum of equal weights, say: the border lies between two values)
+          all_kept = true;
+          border = min(border, word_of(even_at, 0) | 0xffffffffull);
+        } else {
+          tie = !ok;
+        }
       }
     }
   }
@@ -839,7 +849,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       listed = gather() <= (uint32_t)kCap;
     }
     all_kept = !listed;                              // down to min_p
-  } else if (!listed && !tie && !whole && min_p > 0.0 && hi < floor_hi) {
+  } else if (!listed && !tie && !all_kept && !whole && min_p > 0.0 && hi < floor_hi) {
     // not everything above the border has min_p
     if (hi <= floor_lo) {
       all_kept = true;                               // min_p ends the kept tokens above it

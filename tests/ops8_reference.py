@@ -63,3 +63,26 @@ def sample_row(l, u, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
     u = u if u > 0 else 0.0
     k = int((cdf <= u * cdf[-1]).sum())
     return int(kept[min(k, n - 1)]), kept, cdf / cdf[-1]
+
+
+def sample_rows(l, u, T, top_k, top_p, min_p):
+    """Tokens of many rows at once: torch tensors, 64 bits, every parameter a vector."""
+    import torch
+    l = l.double()
+    l = torch.where(l != l, -float("inf"), l)
+    o, ids = torch.sort(l, dim=1, descending=True, stable=True)
+    top = o[:, :1]
+    w = torch.where(o == top, 1.0, torch.exp((o - top) / T.double()[:, None]))
+    rank = torch.arange(l.shape[1], device=l.device)[None]
+    k = top_k.long()[:, None]
+    kept = ((k <= 0) | (rank < k)) & (o > -float("inf"))
+    w = torch.where(kept, w, 0.0)
+    before = torch.nn.functional.pad(w.cumsum(1), (1, 0))
+    p = top_p.double()[:, None]
+    kept &= (p >= 1) | (before[:, :-1] < p * before[:, -1:]) | (rank == 0)
+    m = min_p.double().clamp(max=1)[:, None]
+    kept &= (m <= 0) | (w >= m)
+    mass = torch.zeros_like(w).scatter_(1, ids, torch.where(kept, w, 0.0))
+    cdf = mass.cumsum(1)
+    tok = torch.minimum((cdf <= u.double()[:, None] * cdf[:, -1:]).sum(1), torch.where(mass > 0, rank, -1).amax(1))
+    return torch.where(T >= 2.0 ** -100, tok, ids[:, 0]).int()

@@ -381,6 +381,69 @@ def test_sample_leaves_other_rows_and_reads_strided_logits():
     assert np.array_equal(tok[1:11].cpu().numpy(), _want_tokens(l, u, par))
 
 
+@pytest.mark.parametrize("kind", ["normal", "flat", "ties", "const", "two", "peaky", "masked", "huge", "half_and_half"])
+@pytest.mark.parametrize("V", [3, 140, 2300, 9001, 33000, 122484])
+def test_sample_distributions(kind, V):
+    """Rows of every shape and all combinations of parameters, among them exact ties of a nucleus' mass (half of a whole number of
+    equal weights), nuclei that reach into the last tokens, limits beyond any list, temperatures that leave only the maximum or
+    make all weights equal; unaligned rows."""
+    R = max(8, min(400, 1600000 // V))
+    g = torch.Generator(device=DEV).manual_seed(V + len(kind))
+    rand = lambda: torch.rand(R, V, generator=g, device=DEV)  # noqa: E731
+    x = torch.randn(R, V, generator=g, device=DEV)
+    x = {"normal": lambda: x * 2, "flat": lambda: x * 1e-3, "ties": lambda: (x * 3).round(), "const": lambda: torch.full_like(x, 0.75),
+         "two": lambda: torch.where(rand() < 0.5, 1.0, 0.9999), "peaky": lambda: x * 6,
+         "masked": lambda: torch.where(rand() < 0.9, -float("inf"), x * 2), "huge": lambda: x * 1e30,
+         "half_and_half": lambda: torch.where(torch.arange(V, device=DEV) % 2 == 0, 0.5, -0.25).expand(R, V)}[kind]().clone()
+    x[:, 0] = 0.5
+    l = torch.empty(R, V + 3, device=DEV)[:, V % 4 % 3: V % 4 % 3 + V]
+    l.copy_(x)
+
+    def pick(values, dtype=torch.float32):
+        return torch.tensor(values, device=DEV)[torch.randint(0, len(values), (R,), generator=g, device=DEV)].to(dtype)
+
+    T = pick([0.3, 0.7, 1.0, 1.0, 2.0, 1e-3, 50.0, 1e20])
+    k = pick([0, 0, 0, 1, 2, 20, 50, 100, 128, 200, 257, 300, 700, 1024, 1500, 5000, V], torch.int32)
+    p = pick([1.0, 1.0, 0.9, 0.95, 0.5, 0.5, 0.25, 0.1, 0.999, 1 - 2.0 ** -24, 1e-6])
+    m = pick([0.0, 0.0, 0.0, 1e-6, 1e-3, 0.02, 0.1, 0.5, 1.0])
+    u = torch.rand(R, generator=g, device=DEV)
+    tok = torch.empty(R, dtype=torch.int32, device=DEV)
+    _P().k_sample(l, u, tok, temperature=T, top_k=k, top_p=p, min_p=m)
+    assert torch.equal(tok, ref.sample_rows(l, u, T, k, p, m))
+
+
+def test_offsets_beyond_32_bits():
+    """Logits of more than 2^31 elements (4.5 GB in bf16): the product writes and the sampler reads the rows behind that mark as it
+    does the same rows in a small matrix."""
+    M, N, K = 70001, 32000, 128
+    a, sa, w, sw = _operands(M, N, K, 5, "plain")
+    sa.mul_(1e-3)
+    u = torch.rand(M, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+    out = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    tok = torch.empty(M, dtype=torch.int32, device=DEV)
+    P = _P()
+    P.k_gemm_fp8(a, sa, w, sw, out)
+    k, p = torch.full((M,), 40, dtype=torch.int32, device=DEV), torch.full((M,), 0.9, device=DEV)
+    P.k_sample(out, u, tok, top_k=k, top_p=p)
+    for rows in (slice(0, 300), slice(67050, 67350), slice(M - 300, M)):          # row 67108 is where 2^31 elements end
+        o2, t2 = torch.empty(300, N, dtype=torch.bfloat16, device=DEV), torch.empty(300, dtype=torch.int32, device=DEV)
+        P.k_gemm_fp8(a[rows], sa[rows], w, sw, o2)
+        P.k_sample(o2, u[rows], t2, top_k=k[rows], top_p=p[rows])
+        assert torch.equal(out[rows], o2) and torch.equal(tok[rows], t2)
+
+
+def test_one_scale_for_all():
+    """Scales of the product's operands may be broadcast (strides of 0)."""
+    M, N, K = 300, 520, 640
+    a, sa, w, sw = _operands(M, N, K, 8, "plain")
+    one, two = torch.full((1, 1), 0.5, device=DEV), torch.full((1, 1), 0.25, device=DEV)
+    for rows in (M, 40):
+        o1, o2 = torch.empty(rows, N, device=DEV), torch.empty(rows, N, device=DEV)
+        _P().k_gemm_fp8(a[:rows], one.expand(rows, 5), w, two.expand(5, 5), o1)
+        _P().k_gemm_fp8(a[:rows], torch.full((rows, 5), 0.5, device=DEV), w, torch.full((5, 5), 0.25, device=DEV), o2)
+        assert torch.equal(o1, o2)
+
+
 # ---- all together ---------------------------------------------------------------------------------------------
 
 def _tail(P, b):
