@@ -3,7 +3,7 @@
 // a and w e4m3, blocks of 128 along K, on the 5th-generation tensor cores (tcgen05.mma.kind::f8f6f4, fp32 accumulators).
 //
 // The scales change from block to block of K, so a block's product (four instructions of K = 32) goes to tensor memory by
-// itself and is added, times its scales, to a sum in the registers of the epilogue warps; tensor memory holds the products of
+// itself and is added, times its scales, to a sum in the registers of the adding warps; tensor memory holds the products of
 // two blocks, so that the warps add one while the tensor pipe computes the next.
 #pragma once
 
@@ -28,8 +28,8 @@ struct Args {
 // The weights take the side of the 128 accumulator lanes and NT rows of A the columns, so a pass over the weights costs
 // 128 x NT products per 128 x 128 weights however few rows there are. A tile (128 weight rows x NT rows of A) is one cluster:
 // its S CTAs share out the blocks of K, and join their sums through distributed shared memory, each for its part of the
-// columns, in the order of the ranks (so the result is the same every time). What bounds it: the weights' bytes; a CTA keeps
-// kBytesInFlight of them on their way.
+// columns, in the order of the ranks (so the result is the same every time). What bounds it: the weights' bytes, of
+// which the two CTAs of an SM keep 96 to 160 KB on their way.
 // Warps: 0 loads (TMA), 1 issues the MMAs and owns tensor memory, the others add: warp w reads the lanes 32 (w % 4) .. + 31,
 // with NT = 128 eight of them split the columns.
 template <int NT>
@@ -225,7 +225,8 @@ __global__ void __launch_bounds__(Few<NT>::kThreads) gemm8_few_kernel(const __gr
 // its limit, and took 1.27 of its share of the time.) The adding warps hold 128 sums a thread and fetch 32 columns ahead of the
 // ones they add: they take the registers that the warpgroup of the loads and the MMAs gives up. A warp of its own keeps the
 // scales of the next blocks coming into shared memory (fetched by the adding warps one block ahead they cost 330 of 1220 clocks a
-// block). What bounds it now is the adding: 256 of a block's 512 clocks are the fused multiply-adds alone.
+// block). What bounds it now is the adding: 870 clocks a block, of which the MMAs need 512.
+// M = 16384, N = 6144, K = 1536, bf16 output: 174 us, 1.78 PFLOP/s at the power cap (1.52 GHz).
 // A tile's output is staged whole (64 KB per CTA in bf16, 128 KB in fp32, which leaves three stages for the operands), and stored while
 // the next tile is computed: all CTAs finish their tiles at about the same time, so that the stores come in bursts that memory takes
 // as long for as the tile's products (with half of an fp32 tile staged, the adding warps waited for the other half: M = 4096,

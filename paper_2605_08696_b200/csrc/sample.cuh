@@ -44,10 +44,6 @@ __device__ __forceinline__ uint32_t logit_key(float l) {
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-template <typename T> __device__ __forceinline__ float load_logit(const Args& p, int64_t row, int i) {
-  return to_float(static_cast<const T*>(p.logits)[row * p.stride + i]);
-}
-
 // A warp reads `E` logits per lane at a time, a stretch of 32 E consecutive ids: 16, or 4 where the ids are few (more threads then share
 // a row, and their maxima tell more of it: 7380 rows of 1352 took 394 us with 16, for most of them sorted whole).
 constexpr int kFewIds = 8192;
@@ -393,10 +389,10 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   const bool wide = reinterpret_cast<uintptr_t>(lr) % (4 * sizeof(T)) == 0;
   pdl_wait();
 
-  // f(16 logits, stretch): this thread's of the block's stretches. Loops and bodies are kept short: most of this kernel's code runs
-  // once or twice per row, so that instructions are fetched anew, and bodies unrolled over the 16 cost more than they saved.
+  // f(E logits, stretch): this thread's of the block's stretches. Loops and bodies are kept short: most of this kernel's code runs
+  // once or twice per row, so that its instructions are fetched anew.
   auto id_at = [&](int q, int j) { return q * kStretch + (wide ? 128 * (j >> 2) + 4 * g.lane + (j & 3) : 32 * j + g.lane); };
-  auto each16 = [&](auto&& f) {
+  auto each_lane = [&](auto&& f) {
 #pragma unroll 1
     for (int q = q0 + g.warp; q < q1; q += g.warps) {
       float v[E];
@@ -437,12 +433,15 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   const int top_k = k0 <= 0 || k0 > p.V ? p.V : k0;
   const double top_p = p0 < 1.0f ? (double)fmaxf(p0, 0.0f) : 1.0, min_p = f0 > 0.0f ? (double)fminf(f0, 1.0f) : 0.0, u = u0 > 0.0f ? (double)u0 : 0.0;
   float top = -INFINITY;                             // this thread's largest logit
-  each16([&](const float (&v)[E], int) { top = max3_nan(top, largest(v), top); });
+  each_lane([&](const float (&v)[E], int) { top = max3_nan(top, largest(v), top); });
   if (!(top < INFINITY)) {
     raise_status(p.status, kStatusNonFinite);
     if (top != top) {                                // a NaN masks its token: it fails every comparison
-      top = -INFINITY;
-      each([&](float l, int) { top = fmaxf(top, l); });
+      top = -INFINITY;                               // (over the same ids again: this thread's alone)
+      each_lane([&](const float (&v)[E], int) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) top = fmaxf(top, v[j]);
+      });
     }
   }
   const float l_max = g.max_of(top);
@@ -465,7 +464,6 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   rate64 = fma(rate64, fma(-octave, rate64, 1.0), rate64);
   rate64 = fma(rate64, fma(-octave, rate64, 1.0), rate64);
   const float rate = (float)fmin(rate64, 3e38);
-  auto weight = [&](float l) { return l == l_max ? 1.0f : ex2(fmaxf(l - l_max, -3e38f) * rate); };
   auto weight_of = [&](float l) { return weight64(l, l_max, rate64); };
   // the logit with weight 2^x, as a finite float
   auto logit_at = [&](double x) {
@@ -540,7 +538,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       const float a = t3[0], b = t3[1], c = t3[2];
       float m[4] = {0.f, 0.f, 0.f, 0.f};
       uint32_t k[3] = {0u, 0u, 0u};
-      each16([&](const float (&v)[E], int q) {
+      each_lane([&](const float (&v)[E], int q) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           // (a NaN or minus infinity ends as 0, the maximum as 1; weights under 2^-80 do no harm)
@@ -653,7 +651,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   auto gather = [&]() {
     collect_begin();
     const float from = lo, to = whole ? no_top : hi;
-    each16([&](const float (&v)[E], int q) {
+    each_lane([&](const float (&v)[E], int q) {
       if (!(largest(v) < from)) pick(v, q, from, to);
     });
     return collect_end();

@@ -355,6 +355,23 @@ def test_sample_masked_rows_and_non_finite_logits():
     assert int(st) == 0
 
 
+@pytest.mark.parametrize("V", [1000, 32000])
+def test_sample_with_a_nan_beside_the_largest_logit(V):
+    """One NaN masks its own token and nothing around it, wherever it stands."""
+    R = 64
+    g = torch.Generator(device=DEV).manual_seed(V)
+    l = torch.randn(R, V, generator=g, device=DEV)
+    at = torch.randint(1, V - 1, (R,), generator=g, device=DEV)
+    rows = torch.arange(R, device=DEV)
+    l[rows, at] = 30.0
+    l[rows, at + torch.where(rows % 2 == 0, 1, -1)] = float("nan")
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    tok = torch.empty(R, dtype=torch.int32, device=DEV)
+    for T in (0.0, 1.0):
+        _P().k_sample(l, torch.full((R,), 0.5, device=DEV), tok, temperature=torch.full((R,), T, device=DEV), status=st)
+        assert torch.equal(tok, at.int()) and int(st) == 4
+
+
 def test_sample_odd_parameters():
     """NaN parameters have no effect (temperature: greedy, u: 0); u of 1 or more picks the last token kept; tiny and huge
     temperatures."""
