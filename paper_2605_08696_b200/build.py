@@ -19,7 +19,7 @@ NVCC_FLAGS = [
     "-Xcompiler", "-fPIC", "-cudart", "static",
 ]
 UNITS = ["srm_api.cu", "ops8_api.cu"]      # translation units: the decode library; 8-bit operators and sampling per row
-OBJ_DIR = os.path.join(PKG_DIR, "build")
+OBJ_DIR = os.path.join(PKG_DIR, "_build")
 
 
 def _closure(unit):
