@@ -117,11 +117,16 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   if (rc != SRM_OK) return rc;
   const int64_t n_tiles = (g.N + 127) / 128, kb = (g.K + 127) / 128;
   if ((g.M + 255) / 256 * ((g.N + 255) / 256) > 0x3fffffff) return SRM_ERR_UNSUPPORTED;
-  if (g.M > 256 && g.N > 128) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
+  // The 256 x 256 tiles of the pairs from 65 rows on where they are sixteen or more, from 385 rows on else. us, few / many kernel:
+  // N = 6144, K = 1536 (24 tiles to 256 rows): 100 rows 29 / 21, 256: 38 / 21, 768: 33 / 17; N = 32000, K = 1024: 100 rows 27 / 19, 512: 80 / 29;
+  // N = 1024, K = 4096 (4 tiles): 100 rows 20 / 30, 256: 28 / 37, 384 (8): 27 / 30, 512: 37 / 29.
+  const int64_t pair_tiles = (g.M + 255) / 256 * ((g.N + 255) / 256);
+  if (g.N > 128 && g.M > 64 && (pair_tiles >= 16 || g.M > 384)) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
   const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
   const int64_t m_tiles = (g.M + nt - 1) / nt;
   if (n_tiles > 65535 || m_tiles > 65535) return SRM_ERR_UNSUPPORTED;
-  int ranks = 1;                       // as many as give every SM two CTAs
+  // Ranks for two CTAs per SM. us with / without: N = 1024, K = 4096, 27 rows 16 / 23, 200 rows 26 / 37; N = 6144, K = 1536, 1 row 15 / 16.
+  int ranks = 1;
   while (ranks < 8 && 2 * ranks <= kb && n_tiles * m_tiles * ranks * 2 <= 2 * sms) ranks *= 2;
   if (nt == 16) return launch_few<16, OT>(g, A, a_stride, W, w_stride, ranks, st);
   if (nt == 32) return launch_few<32, OT>(g, A, a_stride, W, w_stride, ranks, st);
@@ -129,8 +134,8 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   return launch_few<128, OT>(g, A, a_stride, W, w_stride, ranks, st);
 }
 
-// Many rows: a block of up to 512 threads each, three per SM (their rows fit in L2 together). Few rows of many ids: a cluster of
-// blocks each, so that a pass is as short as for 32768 ids or fewer.
+// A block of up to 512 threads per row, two per SM; few rows of many ids: a cluster of blocks each, as long as all find room at once.
+// us with / without: 1 row of 131072 20 / 26, 8 rows 42 / 127, 32 rows of 60000 80 / 132.
 template <typename T>
 int launch_sample(const smp::Args& p, cudaStream_t st) {
   int sms = 0;

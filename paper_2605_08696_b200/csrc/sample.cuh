@@ -45,8 +45,8 @@ __device__ __forceinline__ uint32_t logit_key(float l) {
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
 // A warp reads `E` logits per lane at a time, a stretch of 32 E consecutive ids: 16, or 4 where the ids are few (more threads then share
-// a row, and their maxima tell more of it: 7380 rows of 1352 took 394 us with 16, for most of them sorted whole).
-constexpr int kFewIds = 8192;
+// a row, and their maxima tell more of it). us with 16 / 4: 2000 rows of 1352 115 / 61, 4096 rows of 8000 181 / 200, 32 rows of 60000 80 / 185.
+constexpr int kFewIds = 4096;
 constexpr int kMaxStretches = 512;               // 262144 ids
 constexpr int kMaxWarps = 32;
 constexpr int kCap = 1024;                       // tokens that are sorted

@@ -199,7 +199,8 @@ def _gemm_bounds(a, sa, w, sw, out_dtype, extra=None):
 
 SHAPES = [(1, 1, 16), (1, 128, 128), (2, 5, 4096), (3, 257, 144), (7, 96, 2048), (16, 32, 1024), (17, 1000, 272), (33, 136, 6144), (64, 8000, 512),
           (65, 384, 1552), (128, 128, 128), (129, 300, 2064), (200, 2048, 640), (255, 513, 640), (256, 256, 256), (300, 520, 1152), (511, 4096, 512),
-          (520, 1024, 1536), (1000, 264, 96), (1025, 1544, 384), (2100, 2056, 272)]
+          (520, 1024, 1536), (1000, 264, 96), (1025, 1544, 384), (2100, 2056, 272), (65, 4104, 144), (70, 4099, 400), (100, 6144, 656),
+          (384, 2050, 256), (385, 129, 128), (400, 257, 1040), (2000, 100, 272)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
