@@ -487,15 +487,15 @@ int srm_k_prefill_mixer(srm_model* m, int32_t layer, int64_t Bp, int32_t n, cons
  * last block of a row may be shorter), of one row (activations) or of 128 rows (weights): an element stands for its
  * code's value times its block's scale. Scale (i, b) of a matrix lies at d_scale[i * scale_row + b * scale_blk], i
  * counting rows or blocks of 128 rows; the strides are free (columns one after the other, scale_blk the larger one,
- * are the faster order; where scales are read a stride of 0 gives all the same one). Widths are multiples of 16; matrices that are not results of srm_k_gemm_fp8 start on 16-byte
- * boundaries, as do their rows (SRM_ERR_ALIGNMENT). R == 0 or M == 0 does nothing. The calls allocate nothing and can
+ * are the faster order; where scales are read a stride of 0 gives all the same one). Widths are multiples of 16; matrices
+ * that are not results of srm_k_gemm_fp8 start on 16-byte boundaries, as do their rows (SRM_ERR_ALIGNMENT). R == 0 or M == 0 does nothing. The calls allocate nothing and can
  * be captured into a graph; nothing outlives a call. All are asynchronous on `stream`. */
 
 /* RMS norm with the residual's addition, into 8 bits [the norms in front of the feed-forward block and the LM head]:
  *   h = x + delta, rounded to x's type (d_delta NULL: h = x);  y = h / sqrt(mean(h^2) + eps) * g;
  *   per row and block of 128 channels: s = max(amax |y| / 448, 2^-100), q = e4m3(y / s), to nearest even.
- * d_x, d_delta [R, d] each in SRM_DTYPE_FP32, _BF16 or _FP16; d_g float[d]; d_sum [R, d] in x's type takes h (NULL: not
- * stored; may be d_x itself, with the same stride); d_q uint8[R, d]; scales as above. Squares and their sum are fp32: values
+ * d_x, d_delta [R, d] each in SRM_DTYPE_FP32, _BF16 or _FP16; d_g float[d], on a 16-byte boundary; d_sum [R, d] in x's
+ * type takes h (NULL: not stored; may be d_x itself, with the same stride); d_q uint8[R, d]; scales as above. Squares and their sum are fp32: values
  * up to 1e17 in magnitude. A row that holds a NaN or an infinity gets codes and scales that are none. d <= 16384, a
  * multiple of 16 (SRM_ERR_UNSUPPORTED). */
 int srm_k_rms_norm_fp8(int64_t R, int32_t d, const void* d_x, int32_t x_dtype, int64_t x_stride, const void* d_delta,
@@ -510,7 +510,7 @@ int srm_k_quant_fp8(int64_t R, int64_t K, const void* d_x, int32_t x_dtype, int6
  * d_A uint8[M, K] with a scale per row and block (as the two calls above leave it), d_W uint8[N, K] with a scale per
  * 128 x 128 block; a block's sum and the sum over the blocks are fp32. d_out in SRM_DTYPE_FP32 or SRM_DTYPE_BF16 (not with
  * accumulate), rows out_stride apart, aligned to its elements. d_bias float[N] or NULL. d_status (may be NULL): a device
- * word, SRM_STATUS_WAIT_TIMEOUT. A result does not depend on which other rows are computed with it beyond its last bits (the
+ * word, SRM_STATUS_WAIT_TIMEOUT. M and N up to 2^30, K up to 2^20 (SRM_ERR_UNSUPPORTED). A result does not depend on which other rows are computed with it beyond its last bits (the
  * order in which the blocks are added). */
 int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t a_stride, const float* d_sa, int64_t sa_row,
                    int64_t sa_blk, const uint8_t* d_W, int64_t w_stride, const float* d_sw, int64_t sw_row, int64_t sw_blk,

@@ -124,7 +124,8 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   if (g.N > 128 && g.M > 64 && (pair_tiles >= 16 || g.M > 384)) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
   const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
   const int64_t m_tiles = (g.M + nt - 1) / nt;
-  if (n_tiles > 65535 || m_tiles > 65535) return SRM_ERR_UNSUPPORTED;
+  // More tiles than a grid's y or z counts: the pairs walk over theirs in a loop.
+  if (n_tiles > 65535 || m_tiles > 65535) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
   // Ranks for two CTAs per SM. us with / without: N = 1024, K = 4096, 27 rows 16 / 23, 200 rows 26 / 37; N = 6144, K = 1536, 1 row 15 / 16.
   int ranks = 1;
   while (ranks < 8 && 2 * ranks <= kb && n_tiles * m_tiles * ranks * 2 <= 2 * sms) ranks *= 2;
@@ -230,7 +231,7 @@ int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t 
   if ((rc = scales_ok(d_sa, M, kb, sa_row, sa_blk, 0)) != SRM_OK || (rc = scales_ok(d_sw, (N + 127) / 128, kb, sw_row, sw_blk, 0)) != SRM_OK) return rc;
   if (d_bias != nullptr && (rc = floats_ok(d_bias)) != SRM_OK) return rc;
   if (d_out == nullptr || (M > 1 && out_stride < N)) return SRM_ERR_INVALID_ARG;
-  if (!aligned(d_out, (size_t)dtype_bytes(out_dtype))) return SRM_ERR_ALIGNMENT;
+  if (!aligned(d_out, (size_t)dtype_bytes(out_dtype)) || !aligned(d_status, 4)) return SRM_ERR_ALIGNMENT;
   const g8::Args g{M, N, K, d_sa, sa_row, sa_blk, d_sw, sw_row, sw_blk, d_bias, accumulate, d_out, out_stride, d_status};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (out_dtype == SRM_DTYPE_FP32) return launch_gemm8<float>(g, d_A, a_stride, d_W, w_stride, st);

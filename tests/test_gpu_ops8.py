@@ -450,6 +450,18 @@ def test_offsets_beyond_32_bits():
         assert torch.equal(out[rows], o2) and torch.equal(tok[rows], t2)
 
 
+@pytest.mark.parametrize("M,N", [(8390003, 24), (3, 8390003)])
+def test_gemm_of_more_tiles_than_a_grid_counts_in_one_direction(M, N):
+    a, sa, w, sw = _operands(M, N, 16, 6, "plain")
+    out = torch.full((M, N), float("nan"), device=DEV)
+    _P().k_gemm_fp8(a, sa, w, sw, out)
+    for at in (0, 65535 * 128 - 128, max(M, N) - 131):                    # 65535 tiles of 128 end at 8388480
+        m, n = (slice(at, at + 131), slice(0, N)) if M > N else (slice(0, M), slice(at // 128 * 128, at + 131))
+        want, bound = _gemm_bounds(a[m], sa[m], w[n], sw[n.start // 128: -(-n.stop // 128)], torch.float32)
+        assert np.all(np.abs(out[m, n].double().cpu().numpy() - want) <= bound)
+    assert bool(torch.isfinite(out).all())
+
+
 def test_one_scale_for_all():
     """Scales of the product's operands may be broadcast (strides of 0)."""
     M, N, K = 300, 520, 640

@@ -26,10 +26,10 @@ def _quant(**kw):
 
 
 def _gemm(**kw):
-    a = dict(M=2, N=8, K=128, A=A, as_=128, sa=A, sar=1, sab=2, W=A, ws=128, sw=A, swr=1, swb=1, bias=None, acc=0, out=A, ot=0, os=8)
+    a = dict(M=2, N=8, K=128, A=A, as_=128, sa=A, sar=1, sab=2, W=A, ws=128, sw=A, swr=1, swb=1, bias=None, acc=0, out=A, ot=0, os=8, st=None)
     a.update(kw)
     return P.load_library().srm_k_gemm_fp8(*[a[k] for k in ("M", "N", "K", "A", "as_", "sa", "sar", "sab", "W", "ws", "sw", "swr",
-                                                           "swb", "bias", "acc", "out", "ot", "os")], None, None)
+                                                           "swb", "bias", "acc", "out", "ot", "os", "st")], None)
 
 
 def _sample(**kw):
@@ -56,6 +56,7 @@ def _sample(**kw):
     (_gemm, dict(A=A + 1), ALIGNMENT), (_gemm, dict(W=A + 8), ALIGNMENT), (_gemm, dict(as_=136), ALIGNMENT), (_gemm, dict(ws=120), INVALID),
     (_gemm, dict(out=A + 2), ALIGNMENT), (_gemm, dict(out=A + 1, ot=1), ALIGNMENT), (_gemm, dict(os=7), INVALID), (_gemm, dict(sar=-1), INVALID),
     (_gemm, dict(N=200, os=200, swr=-1), INVALID), (_gemm, dict(bias=A + 2), ALIGNMENT), (_gemm, dict(M=0, A=None), OK),
+    (_gemm, dict(M=(1 << 30) + 1), UNSUPPORTED), (_gemm, dict(K=(1 << 20) + 16), UNSUPPORTED), (_gemm, dict(st=A + 2), ALIGNMENT),
     (_sample, dict(R=-1), INVALID), (_sample, dict(V=0), INVALID), (_sample, dict(V=262145, ls=262145), UNSUPPORTED), (_sample, dict(lt=5), INVALID),
     (_sample, dict(l=None), INVALID), (_sample, dict(u=None), INVALID), (_sample, dict(tok=None), INVALID), (_sample, dict(ls=7), INVALID),
     (_sample, dict(l=A + 2), ALIGNMENT), (_sample, dict(l=A + 1, lt=1), ALIGNMENT), (_sample, dict(T=A + 1), ALIGNMENT),
