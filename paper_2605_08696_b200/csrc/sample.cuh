@@ -109,6 +109,10 @@ struct Scratch {
   double box[2];                       // from the leading rank to the others
 };
 
+// Cluster barrier in two halves, for all threads of all blocks.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
 // What a block (or, with CL, a cluster) knows and does together. Reductions use two sets of places in turn, so one barrier each is
 // enough; their order is fixed, so results are the same every time, in every thread.
 template <bool CL>
@@ -378,6 +382,9 @@ template <typename T, bool CL, int E>
 __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int per_rank) {
   constexpr int kStretch = 32 * E;
   pdl_trigger();
+  // A block's shared memory may be reached from others once all blocks of the cluster run: waited for in front of the first reduction,
+  // behind the first pass.
+  if (CL) cluster_arrive();
   __shared__ Scratch s;
   Group<CL> g{s, (int)threadIdx.x, (int)threadIdx.x & 31, (int)threadIdx.x >> 5, (int)blockDim.x >> 5, CL ? (int)blockIdx.x : 0, CL ? (int)gridDim.x : 1};
   const int threads = blockDim.x;
@@ -444,6 +451,7 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
       });
     }
   }
+  if (CL) cluster_wait();
   const float l_max = g.max_of(top);
   if (l_max == -INFINITY) {                          // nothing can be picked
     if (g.tid == 0 && g.rank == 0) { raise_status(p.status, kStatusNonFinite); p.tok[row] = 0; }
