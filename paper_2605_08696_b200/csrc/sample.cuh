@@ -102,6 +102,7 @@ struct Scratch {
   double d[2][kMaxWarps], rank_d[2][kMaxRanks];
   float f[2][kMaxWarps], rank_f[2][kMaxRanks];
   uint32_t n[2][kMaxWarps], rank_n[2][kMaxRanks];
+  uint32_t block_n[kMaxWarps];
   float f4[2][4][kMaxWarps], rank_f4[2][kMaxRanks][4];
   uint32_t n3[2][3][kMaxWarps], rank_n3[2][kMaxRanks][3];
   uint32_t count;
@@ -114,7 +115,8 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // What a block (or, with CL, a cluster) knows and does together. Reductions use two sets of places in turn, so one barrier each is
-// enough; their order is fixed, so results are the same every time, in every thread.
+// enough: who writes a set again has passed the barrier of the reduction between, and so has every reader (of all ranks: only
+// reductions in which they all wait take the sets). Their order is fixed, so results are the same every time, in every thread.
 template <bool CL>
 struct Group {
   Scratch& s;
@@ -146,13 +148,11 @@ struct Group {
     }
     return v;
   }
-  __device__ uint32_t block_max(uint32_t v) {                          // (of this block alone)
-    const int b = turn;
-    turn ^= 1;
+  __device__ uint32_t block_max(uint32_t v) {                          // of this block alone; used once, in places of its own
     v = __reduce_max_sync(0xffffffffu, v);
-    if (lane == 0) s.n[b][warp] = v;
+    if (lane == 0) s.block_n[warp] = v;
     __syncthreads();
-    return __reduce_max_sync(0xffffffffu, lane < warps ? s.n[b][lane] : 0u);
+    return __reduce_max_sync(0xffffffffu, lane < warps ? s.block_n[lane] : 0u);
   }
   __device__ uint32_t min_of(uint32_t v) {
     const int b = turn;

@@ -42,3 +42,22 @@ def test_sampler_waits_for_the_cluster_before_it_reaches_into_another_block():
     for at in (arrive, wait):                        # unconditional in the cluster's kernel: no thread is left out
         assert k[:at].rstrip().endswith("if (CL)")
         assert k[:at].count("{") == k[:at].count("}")
+
+
+def test_sampler_flips_its_sets_of_places_only_where_all_ranks_wait():
+    """Reductions use two sets of places in turn: the one after the next may write a set again, which is safe if every rank has
+    passed a barrier of the whole cluster in between, that of the next one. A reduction of one block alone that flipped the set
+    would leave none between a set's readers and its next writers."""
+    text = _source("sample.cuh")
+    group = _body(text, text.index("struct Group"))
+    members = {m.group(1): _body(group, m.end()) for m in re.finditer(r"__device__ \w+ (\w+)\([^{]*\)\s*(?={)", group)}
+    flips = {name for name, b in members.items() if "turn ^= 1" in b}
+    assert {"max_of", "min_of", "add7", "add64"} <= flips <= set(members)
+    for name in flips:
+        assert "sync_all();" in members[name], name
+        assert len(re.findall(r"\bturn\b", members[name])) == 2      # one set, taken and flipped
+    # and a reduction of the block alone has places that no other one writes
+    own = re.findall(r"\bs\.(\w+)\[warp\] = ", members["block_max"])
+    assert len(own) == 1
+    assert not any(re.search(rf"\bs\.{own[0]}\b", b) for name, b in members.items() if name != "block_max")
+    assert not re.search(rf"\bs\.{own[0]}\b", _sampler())
