@@ -286,7 +286,7 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* boxes = smem + F::kStages * F::kStage;
   float* scales = reinterpret_cast<float*>(boxes + F::kAddWarps * F::kBoxes * F::kBox);
-  uint64_t* full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(scales) + F::kScales);      // leader's: both CTAs' copies of a stage
+  uint64_t* full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(scales) + F::kScales);      // leader's: both CTAs' copies of a stage, their scale warps' word
   uint64_t* empty = full + F::kStages;                                  // per CTA: the stage may be filled again
   uint64_t* tfull = empty + F::kStages;                                 // per CTA [2]: a block's product is there
   uint64_t* tempty = tfull + 2;                                         // leader's [2]: both CTAs' warps have fetched it
@@ -301,7 +301,7 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   const uint32_t rank = cta_rank();
   const uint32_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < F::kStages; ++s) { bar_init(&full[s], 2); bar_init(&empty[s], 1); }
+    for (int s = 0; s < F::kStages; ++s) { bar_init(&full[s], 4); bar_init(&empty[s], 1); }
     for (int a = 0; a < 2; ++a) { bar_init(&tfull[a], 1); bar_init(&tempty[a], 2 * F::kAddWarps); }
     for (int a = 0; a < F::kSlots; ++a) bar_init(&sfull[a], 32);
     bar_init_fence();
@@ -358,7 +358,9 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
   } else if (warp == 2) {
     // A block's scales take the slot of the block kStages + 2 before it, whose sums are done: this block's stage is free, so the MMAs
-    // are past the block kStages before it, and they are never more than two blocks ahead of the sums.
+    // are past the block kStages before it, and they are never more than two blocks ahead of the sums. The block's MMAs wait for this
+    // warp's arrival, which comes when all its lanes have seen the stage free: they could complete the barrier's next phase under it
+    // otherwise (they need no scales, and run ahead of the sums), and the wait by parity would miss its own.
     int stage = 0, at = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -368,7 +370,8 @@ gemm8_many_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       for (int j = 0; j < 4; ++j) sa[j] = g.sa + min((int64_t)(q % m_tiles * 256 + rank * 128 + j * 32 + lane), g.M - 1) * g.sa_row;
       const float* sw = g.sw + (min((int64_t)(q / m_tiles) * 256 + (lane & 1) * 128, g.N - 1) >> 7) * g.sw_row;
       for (int kb = 0; kb < kbs; ++kb) {
-        if (!bar_wait(&empty[stage], phase ^ 1u, g.status)) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, bar_wait(&empty[stage], phase ^ 1u, g.status))) { ok = false; break; }
+        if (lane == 0) bar_arrive(peer_addr(smem_addr(&full[stage]), 0));
         float* to = scales + at * 130;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
