@@ -1,9 +1,10 @@
-"""The 8-bit product of many rows beside other work: short products one after the other on two streams, compared with the 64-bit
-form."""
+"""The 8-bit product of many rows and the sampler's cluster kernels beside other work: short products one after the other on two
+streams, and clusters whose blocks start late and out of step. Every result is compared with the 64-bit form."""
 import numpy as np
 import pytest
 import torch
 
+import ops8_reference as ref
 from test_gpu_ops8 import DEV, _P, _gemm_bounds, _operands
 
 pytestmark = pytest.mark.gpu
@@ -31,3 +32,28 @@ def test_short_products_of_many_rows_on_two_streams(K, out_dtype):
         assert torch.equal(pair[0], pair[1])
         want, bound = _gemm_bounds(*o, out_dtype)
         assert np.all(np.abs(pair[0].double().cpu().numpy() - want) <= bound)
+
+
+@pytest.mark.parametrize("R,V", [(1, 131072), (3, 262144), (9, 60001), (17, 40000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sampler_clusters_beside_other_work(R, V, dtype):
+    """Few rows and long vocabularies (a cluster of blocks each), while another stream keeps the SMs busy."""
+    P = _P()
+    g = torch.Generator(device=DEV).manual_seed(R + V)
+    l = (torch.randn(R, V, generator=g, device=DEV) * 2).to(dtype)
+    busy, side = torch.randn(4096, 4096, device=DEV), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for k, p, m in ((0, 0.9, 0.0), (50, 1.0, 0.0), (50, 0.8, 0.02), (0, 1.0, 0.1), (0, 1.0, 0.0), (1500, 0.95, 0.0), (1, 1.0, 0.0), (20, 0.3, 0.0)):
+        par = [torch.full((R,), 0.8, device=DEV), torch.full((R,), k, dtype=torch.int32, device=DEV), torch.full((R,), p, device=DEV),
+               torch.full((R,), m, device=DEV)]
+        us = [torch.rand(R, generator=g, device=DEV) for _ in range(12)]
+        toks = [torch.empty(R, dtype=torch.int32, device=DEV) for _ in us]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(6):
+                busy = torch.tanh(busy @ busy.t() * 1e-2)
+        for u, tok in zip(us, toks):
+            P.k_sample(l, u, tok, temperature=par[0], top_k=par[1], top_p=par[2], min_p=par[3])
+        torch.cuda.synchronize()
+        for u, tok in zip(us, toks):
+            assert torch.equal(tok, ref.sample_rows(l, u, *par))
