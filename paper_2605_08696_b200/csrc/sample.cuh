@@ -466,8 +466,9 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
     if (CL) g.sync_all();
     return;
   }
-  // T ln 2, and its reciprocal: the fp32 one and two Newton steps (a division would be forty instructions in every warp)
-  const double octave = (double)fminf(T0, 1e38f) * 0.693147180559945309417;
+  // T ln 2, and its reciprocal: the fp32 one and two Newton steps (a division would be forty instructions in every warp). For an infinite
+  // T an octave beyond all differences, and a rate that stays 0: every weight is 1, but those of masked tokens (0 times infinity).
+  const double octave = T0 < INFINITY ? (double)T0 * 0.693147180559945309417 : 1e300;
   double rate64 = (double)(1.0f / (float)octave);
   rate64 = fma(rate64, fma(-octave, rate64, 1.0), rate64);
   rate64 = fma(rate64, fma(-octave, rate64, 1.0), rate64);
@@ -543,14 +544,16 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
   auto sum3 = [&](bool exact, bool list) {
     if (!exact) {
       const bool inf = l_max == INFINITY;
+      const float half_max = 0.5f * l_max, rate2 = 2.0f * rate;
       const float a = t3[0], b = t3[1], c = t3[2];
       float m[4] = {0.f, 0.f, 0.f, 0.f};
       uint32_t k[3] = {0u, 0u, 0u};
       each_lane([&](const float (&v)[E], int q) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          // (a NaN or minus infinity ends as 0, the maximum as 1; weights under 2^-80 do no harm)
-          float w = ex2(fmaxf(v[i] - l_max, -3e38f) * rate);
+          // (halves, whose difference is always finite. A NaN or minus infinity ends as 0, whatever the rate, the maximum as 1; weights
+          // under 2^-80 do no harm)
+          float w = ex2(fmaxf(fmaf(0.5f, v[i], -half_max) * rate2, -INFINITY));
           if (inf) w = v[i] == l_max ? 1.0f : 0.0f;
           m[3] += w;
           if (v[i] >= c) { m[2] += w; ++k[2]; }

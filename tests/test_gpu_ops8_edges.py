@@ -1,0 +1,55 @@
+"""Ends of the ranges that the 8-bit operators and the sampler with parameters per row take, against 64-bit forms."""
+import pytest
+import torch
+
+import ops8_reference as ref
+from test_gpu_ops8 import DEV, _P
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def _pick(g, R, values, dtype=torch.float32):
+    return torch.tensor(values, device=DEV)[torch.randint(0, len(values), (R,), generator=g, device=DEV)].to(dtype)
+
+
+def _tokens(l, u, T, k, p, m):
+    tok = torch.full((l.shape[0],), -7, dtype=torch.int32, device=DEV)
+    _P().k_sample(l, u, tok, temperature=T, top_k=k, top_p=p, min_p=m)
+    return tok
+
+
+# ---- sampling at the highest temperatures -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["equal", "normal", "lowest", "widest"])
+@pytest.mark.parametrize("mask", ["none", "minus_infinity", "nan"])
+@pytest.mark.parametrize("R,V", [(256, 100), (200, 2300), (200, 9001), (2, 100000)])
+def test_sample_at_high_temperatures(R, V, kind, mask):
+    """A masked token (minus infinity, NaN) has no mass at any temperature, up to infinity, where all others have the same; and
+    logits further apart than the largest fp32 number have the weights of their difference."""
+    g = torch.Generator(device=DEV).manual_seed(V + 7 * len(kind) + len(mask))
+    rand = lambda: torch.rand(R, V, generator=g, device=DEV)  # noqa: E731
+    l = {"equal": lambda: torch.full((R, V), 0.75, device=DEV), "normal": lambda: torch.randn(R, V, generator=g, device=DEV) * 3,
+         "lowest": lambda: torch.where(rand() < 0.5, torch.finfo(torch.float32).min, 2.0),
+         "widest": lambda: (rand() * 2 - 1) * torch.finfo(torch.float32).max}[kind]()
+    if mask != "none":
+        l = torch.where(rand() < 0.5, -INF if mask == "minus_infinity" else float("nan"), l)
+        l[:, 0] = 0.75
+    for T in ([1e30, 1e36, 8e36], [2e37, 1e38], [3.4028235e38, INF]):
+        for _ in range(3 if R < 8 else 1):
+            args = (torch.rand(R, generator=g, device=DEV), _pick(g, R, T), _pick(g, R, [0, 0, 0, 20, 60, 1500], torch.int32),
+                    _pick(g, R, [0.1, 0.5, 0.9, 0.9, 0.999, 1.0]), _pick(g, R, [0.0, 0.0, 0.0, 1e-3, 0.5, 1.0]))
+            assert torch.equal(_tokens(l, *args), ref.sample_rows(l, *args))
+
+
+def test_masked_half_of_a_row_at_infinite_temperature():
+    """Fifty tokens of equal weight, 0.9 of their mass: the first 45, whatever stands in the masked places."""
+    l = torch.full((2, 100), 0.75, device=DEV)
+    l[0, 1::2], l[1, 1::2] = -INF, float("nan")
+    n = 4000
+    l = l.repeat_interleave(n, 0)
+    u = torch.linspace(0, 1 - 2.0 ** -24, n, device=DEV).repeat(2)
+    tok = torch.empty(2 * n, dtype=torch.int32, device=DEV)
+    _P().k_sample(l, u, tok, temperature=torch.full((2 * n,), INF, device=DEV), top_p=torch.full((2 * n,), 0.9, device=DEV))
+    for t in tok.view(2, n):
+        assert t.unique().tolist() == list(range(0, 90, 2))
