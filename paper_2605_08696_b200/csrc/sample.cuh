@@ -56,20 +56,26 @@ constexpr int kMaxRanks = 8;
 // of at most 512 weights in a thread's run and two levels of five add 522 roundings (3.2e-5).
 constexpr float kSlack = 5e-5f;
 constexpr double kSlack64 = 1e-11;               // the same for weights and sums in 64 bits
-constexpr double kLeastLog2 = -80.0;             // all weights below 2^-80 together are under 64-bit rounding (2^18 ids)
+constexpr double kLeastLog2 = -80.0;             // all weights below 2^-80 together are under 64-bit rounding (2^18 ids), and outside every nucleus
+constexpr double kNoLog2 = -1076.0;              // below it a weight is 0 in 64 bits. Without a nucleus all others count: u may be 0 (or tiny),
+                                                 // and then falls on the first of them
 constexpr int kRounds = 40;                      // of a search: every other one takes two bits off the distance of lo and hi as keys
 
 // 2^y for y <= 0 in 64 bits: the power of two by the exponent field, the rest by the series of exp to the 12th power of an
 // argument of at most ln 2 / 2 (the remainder is under 2e-16). Rounding to the whole number by adding 1.5 2^52, whose low word then
-// holds it (the conversion instructions have an eighth of the rate).
+// holds it (the conversion instructions have an eighth of the rate). Results below 2^-1000 take their last 128 powers by a product,
+// which rounds where they are denormal.
 __device__ __forceinline__ double pow2_64(double y) {
-  if (!(y > -1000.0)) return 0.0;
+  if (!(y > kNoLog2)) return 0.0;
+  const bool tiny = y < -1000.0;
+  if (tiny) y += 128.0;
   const double shifted = y + 6755399441055744.0, n = shifted - 6755399441055744.0, t = (y - n) * 0.693147180559945309417;
   double s = 1.0 / 479001600;
   s = fma(s, t, 1.0 / 39916800); s = fma(s, t, 1.0 / 3628800); s = fma(s, t, 1.0 / 362880); s = fma(s, t, 1.0 / 40320);
   s = fma(s, t, 1.0 / 5040); s = fma(s, t, 1.0 / 720); s = fma(s, t, 1.0 / 120); s = fma(s, t, 1.0 / 24); s = fma(s, t, 1.0 / 6);
   s = fma(s, t, 0.5); s = fma(s, t, 1.0); s = fma(s, t, 1.0);
-  return __hiloint2double(__double2hiint(s) + (__double2loint(shifted) << 20), __double2loint(s));
+  s = __hiloint2double(__double2hiint(s) + (__double2loint(shifted) << 20), __double2loint(s));
+  return tiny ? s * 0x1p-128 : s;
 }
 
 // Weight of a token in 64 bits; l_max itself (infinite or not) has 1. `rate`: 1 / (T ln 2).
@@ -480,11 +486,12 @@ __global__ void __launch_bounds__(512, 2) sample_kernel(const Args p, const int 
     return v > -3.4e38 ? (float)v : -3.402823466e38f;
   };
   const bool limit_k = top_k < p.V, limit_p = top_p < 1.0;
-  const float least = l_max == INFINITY ? INFINITY : logit_at(kLeastLog2);
+  const float least = l_max == INFINITY ? INFINITY : logit_at(limit_p ? kLeastLog2 : kNoLog2);
   // min_p as logits: surely below, surely above
   float floor_lo = least, floor_hi = least;
   if (min_p > 0.0 && l_max < INFINITY) {
-    const double x = (double)__log2f((float)min_p), v = fma(x, octave, (double)l_max);       // (2^-22 off at most)
+    const bool tiny = min_p < 0x1p-100;              // (2^64 times as much is a normal number)
+    const double x = (double)__log2f((float)(tiny ? min_p * 0x1p64 : min_p)) - (tiny ? 64.0 : 0.0), v = fma(x, octave, (double)l_max);       // (off by 3.6e-7 (1 + |x|) at most)
     const double off = 1e-6 * (fabs(v) + fabs((double)l_max) + octave * (1.0 - x));
     floor_lo = fmaxf(least, v - off > -3.4e38 ? (float)(v - off) : least);
     floor_hi = fmaxf(least, v + off > -3.4e38 ? (float)(v + off) : least);

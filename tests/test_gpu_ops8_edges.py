@@ -53,3 +53,20 @@ def test_masked_half_of_a_row_at_infinite_temperature():
     _P().k_sample(l, u, tok, temperature=torch.full((2 * n,), INF, device=DEV), top_p=torch.full((2 * n,), 0.9, device=DEV))
     for t in tok.view(2, n):
         assert t.unique().tolist() == list(range(0, 90, 2))
+
+
+# ---- random numbers at and next to zero ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("R,V", [(300, 100), (200, 2300), (200, 9001), (2, 100000)])
+def test_sample_with_random_numbers_near_zero(R, V, dtype):
+    """u = 0 picks the lowest id that is kept, however little it weighs (as long as that is a number in 64 bits), and a tiny u the
+    id that its mass falls on."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    l = (torch.randn(R, V, generator=g, device=DEV) * _pick(g, R, [2.0, 15.0, 40.0])[:, None]).to(dtype)
+    l[:, 3] = -INF
+    for us in ([0.0], [1e-45, 1e-40, 1e-36, 1e-30], [1e-25, 1e-20, 2.0 ** -40, 2.0 ** -24]):
+        for _ in range(4 if R < 8 else 1):
+            args = (_pick(g, R, us), _pick(g, R, [0.3, 1.0, 3.0]), _pick(g, R, [0, 0, 20, 50, 300, 1500, V], torch.int32),
+                    _pick(g, R, [1.0, 1.0, 1.0, 0.9]), _pick(g, R, [0.0, 0.0, 1e-40, 1e-36, 1e-30, 1e-10]))
+            assert torch.equal(_tokens(l, *args), ref.sample_rows(l, *args))
