@@ -487,7 +487,8 @@ int srm_k_prefill_mixer(srm_model* m, int32_t layer, int64_t Bp, int32_t n, cons
  * last block of a row may be shorter), of one row (activations) or of 128 rows (weights): an element stands for its
  * code's value times its block's scale. Scale (i, b) of a matrix lies at d_scale[i * scale_row + b * scale_blk], i
  * counting rows or blocks of 128 rows; the strides are free (columns one after the other, scale_blk the larger one,
- * are the faster order; where scales are read a stride of 0 gives all the same one). Widths are multiples of 16; matrices
+ * are the faster order; where scales are read a stride of 0 gives all the same one; strides that put two scales that are
+ * written into one place are refused). Widths are multiples of 16; matrices
  * that are not results of srm_k_gemm_fp8 start on 16-byte boundaries, as do their rows (SRM_ERR_ALIGNMENT). R == 0 or M == 0 does nothing. The calls allocate nothing and can
  * be captured into a graph; nothing outlives a call. All are asynchronous on `stream`. */
 

@@ -1,5 +1,7 @@
 // C ABI of the 8-bit operators and of the sampler with parameters per row (see include/srm.h for the contract): argument
 // checking and launches.
+#include <numeric>
+
 #include "host.cuh"
 
 #include "gemm8.cuh"
@@ -26,9 +28,19 @@ int rows_ok(const void* p, int64_t rows, int64_t cols, int64_t stride, int64_t e
   return SRM_OK;
 }
 int floats_ok(const void* p) { return p == nullptr ? SRM_ERR_INVALID_ARG : !aligned(p, 4) ? SRM_ERR_ALIGNMENT : SRM_OK; }
-// Scales of a matrix, rows x blks of them: written ones each in a place of their own, read ones with any stride from 0.
-int scales_ok(const float* p, int64_t rows, int64_t blks, int64_t row, int64_t blk, int64_t least) {
-  return (rows > 1 && row < least) || (blks > 1 && blk < least) ? SRM_ERR_INVALID_ARG : floats_ok(p);
+// Scales of a matrix, rows x blks of them. Written ones each in a place of its own: places i row + b blk of two scales are the same where
+// their rows are a multiple of blk / gcd apart and their blocks the same multiple of row / gcd.
+int written_scales_ok(const float* p, int64_t rows, int64_t blks, int64_t row, int64_t blk) {
+  if ((rows > 1 && row < 1) || (blks > 1 && blk < 1)) return SRM_ERR_INVALID_ARG;
+  if (rows > 1 && blks > 1) {
+    const int64_t g = std::gcd(row, blk);
+    if (blk / g < rows && row / g < blks) return SRM_ERR_INVALID_ARG;
+  }
+  return floats_ok(p);
+}
+// Read ones with any stride from 0.
+int read_scales_ok(const float* p, int64_t rows, int64_t blks, int64_t row, int64_t blk) {
+  return (rows > 1 && row < 0) || (blks > 1 && blk < 0) ? SRM_ERR_INVALID_ARG : floats_ok(p);
 }
 
 constexpr int64_t kMaxGrid = 0x7fffffff;
@@ -186,7 +198,7 @@ int srm_k_rms_norm_fp8(int64_t R, int32_t d, const void* d_x, int32_t x_dtype, i
   if (d_sum != nullptr && (rc = rows_ok(d_sum, R, d, sum_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
   if ((rc = rows_ok(d_q, R, d, q_stride, 1)) != SRM_OK) return rc;
   if ((rc = rows_ok(d_g, 1, d, d, 4)) != SRM_OK) return rc;
-  if ((rc = scales_ok(d_scale, R, (d + 127) / 128, scale_row, scale_blk, 1)) != SRM_OK) return rc;
+  if ((rc = written_scales_ok(d_scale, R, (d + 127) / 128, scale_row, scale_blk)) != SRM_OK) return rc;
   const q8::NormArgs p{R, d, d_x, x_stride, d_delta, delta_stride, d_g, eps, d_sum, sum_stride, d_q, q_stride, d_scale, scale_row, scale_blk};
   return with_type(x_dtype, [&](auto x) {
     return with_type(d_delta != nullptr ? delta_dtype : SRM_DTYPE_FP32,
@@ -205,7 +217,7 @@ int srm_k_quant_fp8(int64_t R, int64_t K, const void* d_x, int32_t x_dtype, int6
   int rc;
   if ((rc = rows_ok(d_x, R, K, x_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
   if ((rc = rows_ok(d_q, R, K, q_stride, 1)) != SRM_OK) return rc;
-  if ((rc = scales_ok(d_scale, (R + block_rows - 1) / block_rows, kb, scale_row, scale_blk, 1)) != SRM_OK) return rc;
+  if ((rc = written_scales_ok(d_scale, (R + block_rows - 1) / block_rows, kb, scale_row, scale_blk)) != SRM_OK) return rc;
   const q8::QuantArgs p{R, K, d_x, x_stride, d_q, q_stride, d_scale, scale_row, scale_blk};
   return with_type(x_dtype, [&](auto x) -> int {
     using XT = decltype(x);
@@ -228,7 +240,7 @@ int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t 
   if ((rc = rows_ok(d_A, M, K, a_stride, 1)) != SRM_OK) return rc;
   if ((rc = rows_ok(d_W, N, K, w_stride, 1)) != SRM_OK) return rc;
   const int64_t kb = (K + 127) / 128;
-  if ((rc = scales_ok(d_sa, M, kb, sa_row, sa_blk, 0)) != SRM_OK || (rc = scales_ok(d_sw, (N + 127) / 128, kb, sw_row, sw_blk, 0)) != SRM_OK) return rc;
+  if ((rc = read_scales_ok(d_sa, M, kb, sa_row, sa_blk)) != SRM_OK || (rc = read_scales_ok(d_sw, (N + 127) / 128, kb, sw_row, sw_blk)) != SRM_OK) return rc;
   if (d_bias != nullptr && (rc = floats_ok(d_bias)) != SRM_OK) return rc;
   if (d_out == nullptr || (M > 1 && out_stride < N)) return SRM_ERR_INVALID_ARG;
   if (!aligned(d_out, (size_t)dtype_bytes(out_dtype)) || !aligned(d_status, 4)) return SRM_ERR_ALIGNMENT;

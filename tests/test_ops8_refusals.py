@@ -1,0 +1,30 @@
+"""Calls of the 8-bit operators whose results would fall on one another. No GPU."""
+import itertools
+
+import pytest
+
+import paper_2605_08696_b200 as P
+from test_ops8_host import A, INVALID, _gemm, _norm, _quant
+
+BAD_ADDRESS = A + 2               # refused for its alignment, which is looked at after the strides: nothing is launched
+
+
+def _overlap(rows, blks, row, blk):
+    places = [i * row + b * blk for i, b in itertools.product(range(rows), range(blks))]
+    return len(set(places)) < len(places)
+
+
+@pytest.mark.parametrize("rows,blks", [(1, 1), (1, 3), (2, 1), (2, 2), (2, 3), (3, 2), (4, 5), (7, 3)])
+def test_written_scales_have_a_place_each(rows, blks):
+    """Row and block strides that put two scales into one place are refused, all others are taken."""
+    K = 128 * blks
+    refused = 0
+    for row, blk in itertools.product(range(1, 9), repeat=2):
+        want = INVALID if _overlap(rows, blks, row, blk) else P.ERR_ALIGNMENT
+        refused += want == INVALID
+        assert _norm(R=rows, d=K, xs=K, qs=K, s=BAD_ADDRESS, sr=row, sb=blk) == want, (row, blk)
+        assert _quant(R=rows, K=K, xs=K, qs=K, s=BAD_ADDRESS, sr=row, sb=blk) == want, (row, blk)
+        assert _quant(R=128 * rows - 5, K=K, xs=K, qs=K, br=128, s=BAD_ADDRESS, sr=row, sb=blk) == want, (row, blk)
+        # scales that are read may share places
+        assert _gemm(M=rows, K=K, as_=K, ws=K, sa=BAD_ADDRESS, sar=row, sab=blk) == P.ERR_ALIGNMENT
+    assert (refused > 0) == (rows > 1 and blks > 1)
