@@ -195,6 +195,7 @@ int srm_k_rms_norm_fp8(int64_t R, int32_t d, const void* d_x, int32_t x_dtype, i
   int rc;
   if ((rc = rows_ok(d_x, R, d, x_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
   if (d_delta != nullptr && (rc = rows_ok(d_delta, R, d, delta_stride, dtype_bytes(delta_dtype))) != SRM_OK) return rc;
+  if (d_sum == d_x && R > 1 && sum_stride != x_stride) return SRM_ERR_INVALID_ARG;      // (a row's sums over another row's x)
   if (d_sum != nullptr && (rc = rows_ok(d_sum, R, d, sum_stride, dtype_bytes(x_dtype))) != SRM_OK) return rc;
   if ((rc = rows_ok(d_q, R, d, q_stride, 1)) != SRM_OK) return rc;
   if ((rc = rows_ok(d_g, 1, d, d, 4)) != SRM_OK) return rc;

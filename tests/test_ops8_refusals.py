@@ -28,3 +28,10 @@ def test_written_scales_have_a_place_each(rows, blks):
         # scales that are read may share places
         assert _gemm(M=rows, K=K, as_=K, ws=K, sa=BAD_ADDRESS, sar=row, sab=blk) == P.ERR_ALIGNMENT
     assert (refused > 0) == (rows > 1 and blks > 1)
+
+
+def test_a_stored_sum_in_place_of_x_has_x_s_stride():
+    kw = dict(x=A, xs=256, dl=A + (1 << 20), ds=128, s=BAD_ADDRESS)
+    assert _norm(h=A, hs=256, **kw) == P.ERR_ALIGNMENT
+    assert _norm(h=A, hs=128, **kw) == INVALID
+    assert _norm(R=1, h=A, hs=128, **kw) == P.ERR_ALIGNMENT      # a single row has no stride
