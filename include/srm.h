@@ -496,9 +496,10 @@ int srm_k_prefill_mixer(srm_model* m, int32_t layer, int64_t Bp, int32_t n, cons
  *   h = x + delta, rounded to x's type (d_delta NULL: h = x);  y = h / sqrt(mean(h^2) + eps) * g;
  *   per row and block of 128 channels: s = max(amax |y| / 448, 2^-100), q = e4m3(y / s), to nearest even.
  * d_x, d_delta [R, d] each in SRM_DTYPE_FP32, _BF16 or _FP16; d_g float[d], on a 16-byte boundary; d_sum [R, d] in x's
- * type takes h (NULL: not stored; may be d_x itself, with the same stride); d_q uint8[R, d]; scales as above. Squares and their sum are fp32: values
- * up to 1e17 in magnitude. A row that holds a NaN or an infinity gets codes and scales that are none. d <= 16384, a
- * multiple of 16 (SRM_ERR_UNSUPPORTED). */
+ * type takes h (NULL: not stored; may be d_x itself, with the same stride); d_q uint8[R, d]; scales as above. Squares and their
+ * sum are fp32: magnitudes up to 1e17, and where eps is 0 rows with a root mean square of 1e-17 or more. A row that holds a NaN
+ * or an infinity, or whose squares sum up to one, gets NaN codes and NaN scales throughout, and so does a row of zeros where
+ * eps is 0. d <= 16384, a multiple of 16 (SRM_ERR_UNSUPPORTED). */
 int srm_k_rms_norm_fp8(int64_t R, int32_t d, const void* d_x, int32_t x_dtype, int64_t x_stride, const void* d_delta,
                        int32_t delta_dtype, int64_t delta_stride, const float* d_g, float eps, void* d_sum, int64_t sum_stride,
                        uint8_t* d_q, int64_t q_stride, float* d_scale, int64_t scale_row, int64_t scale_blk, void* stream);

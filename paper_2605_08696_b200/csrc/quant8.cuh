@@ -117,7 +117,8 @@ __global__ void rms_norm_fp8_kernel(const NormArgs p) {
     __syncthreads();
     ss = warp_sum(lane < warps ? part[lane] : 0.f);
   }
-  const float rstd = rsqrtf(ss / (float)p.d + p.eps);
+  // (an infinite sum would leave zeros in every block but the infinity's own, and in all of them where only squares were too large)
+  const float rstd = ss < INFINITY ? rsqrtf(ss / (float)p.d + p.eps) : __int_as_float(0x7fffffff);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int i = j * blockDim.x + tid;

@@ -1,9 +1,10 @@
 """Ends of the ranges that the 8-bit operators and the sampler with parameters per row take, against 64-bit forms."""
+import numpy as np
 import pytest
 import torch
 
 import ops8_reference as ref
-from test_gpu_ops8 import DEV, _P
+from test_gpu_ops8 import DEV, NORM_REL, _P, _check_codes, _codes
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -70,3 +71,45 @@ def test_sample_with_random_numbers_near_zero(R, V, dtype):
             args = (_pick(g, R, us), _pick(g, R, [0.3, 1.0, 3.0]), _pick(g, R, [0, 0, 20, 50, 300, 1500, V], torch.int32),
                     _pick(g, R, [1.0, 1.0, 1.0, 0.9]), _pick(g, R, [0.0, 0.0, 1e-40, 1e-36, 1e-30, 1e-10]))
             assert torch.equal(_tokens(l, *args), ref.sample_rows(l, *args))
+
+
+# ---- RMS norm: rows that are not finite, and the least rows without eps ---------------------------------------------
+
+@pytest.mark.parametrize("d", [16, 384, 5008, 16384])
+@pytest.mark.parametrize("xt", [torch.float32, torch.bfloat16, torch.float16])
+def test_rms_norm_of_rows_that_are_not_finite(d, xt):
+    """A NaN, an infinity, or squares beyond fp32 make the whole row's codes and scales NaN, and no other row's."""
+    g = torch.Generator(device=DEV).manual_seed(d)
+    x = torch.randn(9, d, generator=g, device=DEV).to(xt)
+    delta = torch.randn(9, d, generator=g, device=DEV)
+    x[1, d - 1], x[2, 0], x[3, d // 2] = INF, -INF, float("nan")
+    delta[5, 7] = INF
+    x[6, 3], delta[6, 3] = 6e4, 6e4                          # beyond fp16, a value like others in the other types
+    delta[7, 1] = 1e25                                       # its square is beyond fp32 (and it is beyond fp16)
+    w = torch.randn(d, generator=g, device=DEV)
+    kb = -(-d // 128)
+    q, s, h = torch.empty(9, d, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(9, kb, device=DEV), torch.empty_like(x)
+    _P().k_rms_norm_fp8(x, w, q, s, delta=delta, sum_out=h, eps=1e-5)
+    bad = [1, 2, 3, 5, 7] + ([6] if xt == torch.float16 else [])
+    good = [r for r in range(9) if r not in bad]
+    assert torch.equal(h.nan_to_num(nan=1.5), (x.float() + delta).to(xt).nan_to_num(nan=1.5))
+    assert bool(((q.view(torch.uint8)[bad] & 127) == 127).all()) and bool(s[bad].isnan().all())
+    want = ref.rms_norm(h[good].double().cpu().numpy(), w.double().cpu().numpy(), float(np.float32(1e-5)))
+    _check_codes(_codes(q[good].view(torch.uint8)), s[good].double().cpu().numpy(), want, ref.block_scales(want, 1), 1, NORM_REL)
+
+
+@pytest.mark.parametrize("d", [16, 400, 16384])
+@pytest.mark.parametrize("rms", [1e-17, 1e-12, 1.0, 1e16])
+def test_rms_norm_without_eps(d, rms):
+    """eps = 0: rows with a root mean square from 1e-17 on, values spread over twelve powers of ten, are as exact as others (below
+    that squares leave fp32's range); a row of zeros has no norm."""
+    g = torch.Generator(device=DEV).manual_seed(d + 1)
+    x = torch.randn(5, d, generator=g, device=DEV).double() * 10.0 ** (-12 * torch.rand(5, d, generator=g, device=DEV).double())
+    x = (x / (x * x).mean(1, keepdim=True).sqrt() * (1.001 * rms)).clamp(-1e17, 1e17).float()
+    x[4] = 0
+    w = torch.randn(d, generator=g, device=DEV)
+    q, s = torch.empty(5, d, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(5, -(-d // 128), device=DEV)
+    _P().k_rms_norm_fp8(x, w, q, s, eps=0.0)
+    assert bool(((q.view(torch.uint8)[4] & 127) == 127).all()) and bool(s[4].isnan().all())
+    want = ref.rms_norm(x[:4].double().cpu().numpy(), w.double().cpu().numpy(), 0.0)
+    _check_codes(_codes(q[:4].view(torch.uint8)), s[:4].double().cpu().numpy(), want, ref.block_scales(want, 1), 1, NORM_REL)
