@@ -512,8 +512,9 @@ int srm_k_quant_fp8(int64_t R, int64_t K, const void* d_x, int32_t x_dtype, int6
  * d_A uint8[M, K] with a scale per row and block (as the two calls above leave it), d_W uint8[N, K] with a scale per
  * 128 x 128 block; a block's sum and the sum over the blocks are fp32. d_out in SRM_DTYPE_FP32 or SRM_DTYPE_BF16 (not with
  * accumulate), rows out_stride apart, aligned to its elements. d_bias float[N] or NULL. d_status (may be NULL): a device
- * word, SRM_STATUS_WAIT_TIMEOUT. M and N up to 2^30, K up to 2^20 (SRM_ERR_UNSUPPORTED). A result does not depend on which other rows are computed with it beyond its last bits (the
- * order in which the blocks are added). */
+ * word, SRM_STATUS_WAIT_TIMEOUT. M and N up to 2^30, fewer than 2^30 tiles of 256 x 256 (2^46 elements of output), K up to 2^20
+ * (SRM_ERR_UNSUPPORTED). A result does not depend on which other rows are computed with it beyond its last bits (the order in
+ * which the blocks are added). */
 int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t a_stride, const float* d_sa, int64_t sa_row,
                    int64_t sa_blk, const uint8_t* d_W, int64_t w_stride, const float* d_sw, int64_t sw_row, int64_t sw_blk,
                    const float* d_bias, int32_t accumulate, void* d_out, int32_t out_dtype, int64_t out_stride, uint32_t* d_status,

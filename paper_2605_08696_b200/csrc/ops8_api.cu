@@ -128,7 +128,6 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   const int rc = device_sm_count(&sms);
   if (rc != SRM_OK) return rc;
   const int64_t n_tiles = (g.N + 127) / 128, kb = (g.K + 127) / 128;
-  if ((g.M + 255) / 256 * ((g.N + 255) / 256) > 0x3fffffff) return SRM_ERR_UNSUPPORTED;
   // The 256 x 256 tiles of the pairs from 65 rows on where they are sixteen or more, from 385 rows on else. us, few / many kernel:
   // N = 6144, K = 1536 (24 tiles to 256 rows): 100 rows 29 / 21, 256: 38 / 21, 768: 33 / 17; N = 32000, K = 1024: 100 rows 27 / 19, 512: 80 / 29;
   // N = 1024, K = 4096 (4 tiles): 100 rows 20 / 30, 256: 28 / 37, 384 (8): 27 / 30, 512: 37 / 29.
@@ -236,6 +235,7 @@ int srm_k_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* d_A, int64_t 
   if (M < 0 || N < 1 || K < 1 || (accumulate != 0 && accumulate != 1)) return SRM_ERR_INVALID_ARG;
   if (out_dtype != SRM_DTYPE_FP32 && out_dtype != SRM_DTYPE_BF16) return SRM_ERR_INVALID_ARG;
   if (K % 16 || K > (1 << 20) || M > (1 << 30) || N > (1 << 30) || (accumulate && out_dtype != SRM_DTYPE_FP32)) return SRM_ERR_UNSUPPORTED;
+  if ((M + 255) / 256 * ((N + 255) / 256) > 0x3fffffff) return SRM_ERR_UNSUPPORTED;      // (tiles are counted in 32 bits)
   if (M == 0) return SRM_OK;
   int rc;
   if ((rc = rows_ok(d_A, M, K, a_stride, 1)) != SRM_OK) return rc;

@@ -35,3 +35,12 @@ def test_a_stored_sum_in_place_of_x_has_x_s_stride():
     assert _norm(h=A, hs=256, **kw) == P.ERR_ALIGNMENT
     assert _norm(h=A, hs=128, **kw) == INVALID
     assert _norm(R=1, h=A, hs=128, **kw) == P.ERR_ALIGNMENT      # a single row has no stride
+
+
+def test_a_product_of_more_tiles_than_are_counted_is_refused_before_anything_else():
+    """2^30 tiles of 256 x 256 and more (2^46 elements of output)."""
+    kw = dict(as_=128, ws=128, K=128, st=BAD_ADDRESS)
+    M, N = 1 << 23, (1 << 23) - 256
+    assert _gemm(M=M, N=N, os=N, **kw) == P.ERR_ALIGNMENT        # (2^15 x (2^15 - 1) tiles: the status word's address comes next)
+    assert _gemm(M=M, N=N + 1, os=N + 1, **kw) == P.ERR_UNSUPPORTED
+    assert _gemm(M=1 << 30, N=1 << 30, os=1 << 30, **kw) == P.ERR_UNSUPPORTED
