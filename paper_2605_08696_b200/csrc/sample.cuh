@@ -55,7 +55,9 @@ constexpr int kMaxRanks = 8;
 // their product are rounded once each, which moves a weight 2^x by 3 |x| 2^-24 ln 2 (|x| <= 80: 1.0e-5), ex2 by 2^-22, and the sums
 // of at most 512 weights in a thread's run and two levels of five add 522 roundings (3.2e-5).
 constexpr float kSlack = 5e-5f;
-constexpr double kSlack64 = 1e-11;               // the same for weights and sums in 64 bits
+// The same for weights and sums in 64 bits: the difference, 1 / (T ln 2) and their product are off by 2^-51 together, which moves a weight
+// 2^x by |x| 2^-51 ln 2 (|x| <= 80: 2.5e-14), the series and its evaluation by 2e-15, and 530 sums by 5.9e-14.
+constexpr double kSlack64 = 1e-13;
 constexpr double kLeastLog2 = -80.0;             // all weights below 2^-80 together are under 64-bit rounding (2^18 ids), and outside every nucleus
 constexpr double kNoLog2 = -1076.0;              // below it a weight is 0 in 64 bits. Without a nucleus all others count: u may be 0 (or tiny),
                                                  // and then falls on the first of them

@@ -113,3 +113,40 @@ def test_rms_norm_without_eps(d, rms):
     assert bool(((q.view(torch.uint8)[4] & 127) == 127).all()) and bool(s[4].isnan().all())
     want = ref.rms_norm(x[:4].double().cpu().numpy(), w.double().cpu().numpy(), 0.0)
     _check_codes(_codes(q[:4].view(torch.uint8)), s[:4].double().cpu().numpy(), want, ref.block_scales(want, 1), 1, NORM_REL)
+
+
+# ---- a nucleus that ends a few 1e-12 of the mass beside a group of equal logits -------------------------------------
+
+def _close_row(nA, nB, V, gap):
+    """Logits of nA tokens at 0, nB at -1 and a few near -16, and a top_p, so that the first group misses top_p's part of the whole
+    mass by `gap` of the whole (negative: exceeds it): what two exponentials in 64 bits tell apart."""
+    w = np.exp(-1.0)
+    p = np.float32(nA / (nA + nB * w))
+    while float(p) * (nA + nB * w) > nA * (1 - 1e-8):
+        p = np.nextafter(p, np.float32(0))
+    total = nA / (float(p) - gap)                    # nA = (p - gap) total
+    nC = 50
+    c = np.float32(np.log((total - nA - nB * w) / nC))
+    l = np.full(V, -np.inf, np.float32)
+    l[: 2 * nA: 2] = 0                               # ids of the first group lie below the second's
+    l[2 * nA: 2 * nA + nB] = -1
+    l[V - nC:] = c
+    total = nA + nB * w + nC * np.exp(float(c))
+    return l, p, (float(p) * total - nA) / total
+
+
+@pytest.mark.parametrize("nA,nB,V", [(1500, 3000, 9001), (2000, 1200, 33000), (5000, 20000, 120000)])
+def test_sample_decides_borders_to_64_bits(nA, nB, V):
+    rows = [_close_row(nA, nB, V, gap) for gap in (4e-12, -4e-12, 1e-12, -1e-12)]
+    for _, _, gap in rows:
+        assert 5e-13 < abs(gap) < 8e-12
+    l = torch.from_numpy(np.stack([r[0] for r in rows])).to(DEV)
+    R = len(rows)
+    p, u = torch.tensor([float(r[1]) for r in rows], device=DEV), torch.full((R,), 1 - 2.0 ** -24, device=DEV)
+    one, none, k = torch.ones(R, device=DEV), torch.zeros(R, device=DEV), torch.zeros(R, dtype=torch.int32, device=DEV)
+    # the last token kept: the first id of the second group where the first one's mass is too little, else the first group's last
+    want = torch.tensor([2 * nA if r[2] > 0 else 2 * nA - 2 for r in rows], dtype=torch.int32, device=DEV)
+    assert torch.equal(ref.sample_rows(l, u, one, k, p, none), want)
+    for n in (1, 100):                               # both launch forms for the longer rows
+        ln, un, pn, on, zn, kn = (t.repeat_interleave(n, 0) for t in (l, u, p, one, none, k))
+        assert torch.equal(_tokens(ln, un, on, kn, pn, zn), want.repeat_interleave(n))
