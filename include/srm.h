@@ -488,11 +488,12 @@ int srm_k_prefill_mixer(srm_model* m, int32_t layer, int64_t Bp, int32_t n, cons
  * code's value times its block's scale. Scale (i, b) of a matrix lies at d_scale[i * scale_row + b * scale_blk], i
  * counting rows or blocks of 128 rows; the strides are free (columns one after the other, scale_blk the larger one,
  * are the faster order; where scales are read a stride of 0 gives all the same one; strides that put two scales that are
- * written into one place are refused). Widths are multiples of 16; matrices
- * that are not results of srm_k_gemm_fp8 start on 16-byte boundaries, as do their rows (SRM_ERR_ALIGNMENT). R == 0 or M == 0 does nothing. The calls allocate nothing and can
+ * written into one place are refused). Widths are multiples of 16; matrices that are not results of srm_k_gemm_fp8 start on
+ * 16-byte boundaries, as do their rows (SRM_ERR_ALIGNMENT). R == 0 or M == 0 does nothing. The calls allocate nothing and can
  * be captured into a graph; nothing outlives a call. All are asynchronous on `stream`. */
 
-/* RMS norm with the residual's addition, into 8 bits [the norms in front of the feed-forward block and the LM head]:
+/* RMS norm with the residual's addition, into 8 bits. (The models of this library norm with a LayerNorm, srm_k_final_norm; their
+ * activations go through the next call. This one is for a caller's own blocks.)
  *   h = x + delta, rounded to x's type (d_delta NULL: h = x);  y = h / sqrt(mean(h^2) + eps) * g;
  *   per row and block of 128 channels: s = max(amax |y| / 448, 2^-100), q = e4m3(y / s), to nearest even.
  * d_x, d_delta [R, d] each in SRM_DTYPE_FP32, _BF16 or _FP16; d_g float[d], on a 16-byte boundary; d_sum [R, d] in x's

@@ -225,8 +225,9 @@ __global__ void __launch_bounds__(Few<NT>::kThreads) gemm8_few_kernel(const __gr
 // its limit, and took 1.27 of its share of the time.) The adding warps hold 128 sums a thread and fetch 32 columns ahead of the
 // ones they add: they take the registers that the warpgroup of the loads and the MMAs gives up. A warp of its own keeps the
 // scales of the next blocks coming into shared memory (fetched by the adding warps one block ahead they cost 330 of 1220 clocks a
-// block). What bounds it now is the adding: 870 clocks a block, of which the MMAs need 512.
-// M = 16384, N = 6144, K = 1536, bf16 output: 174 us, 1.78 PFLOP/s at the power cap (1.52 GHz).
+// block). What bounds it now is the adding: 870 clocks a block, of which the MMAs need 512. It is a chain of waits rather than a count of
+// instructions: 128 scalar multiply-adds of two warps per scheduler are 256 issue slots, and half of all slots stay empty.
+// M = 16384, N = 6144, K = 1536, bf16 output: 175 to 177 us a pass among others, 1.75 PFLOP/s at the power cap (1.52 GHz).
 // A tile's output is staged whole (64 KB per CTA in bf16, 128 KB in fp32, which leaves three stages for the operands), and stored while
 // the next tile is computed: all CTAs finish their tiles at about the same time, so that the stores come in bursts that memory takes
 // as long for as the tile's products (with half of an fp32 tile staged, the adding warps waited for the other half: M = 4096,

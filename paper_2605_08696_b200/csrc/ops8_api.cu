@@ -128,16 +128,18 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
   const int rc = device_sm_count(&sms);
   if (rc != SRM_OK) return rc;
   const int64_t n_tiles = (g.N + 127) / 128, kb = (g.K + 127) / 128;
-  // The 256 x 256 tiles of the pairs from 65 rows on where they are sixteen or more, from 385 rows on else. us, few / many kernel:
-  // N = 6144, K = 1536 (24 tiles to 256 rows): 100 rows 29 / 21, 256: 38 / 21, 768: 33 / 17; N = 32000, K = 1024: 100 rows 27 / 19, 512: 80 / 29;
-  // N = 1024, K = 4096 (4 tiles): 100 rows 20 / 30, 256: 28 / 37, 384 (8): 27 / 30, 512: 37 / 29.
+  // The 256 x 256 tiles of the pairs from 65 rows on where they are sixteen or more, from 385 rows on else. us (events around a launch, L2
+  // flushed before it), few / many kernel: N = 6144, K = 1536, bf16 out (24 tiles to 256 rows): 100 rows 25 / 16, 256: 35 / 16, 768: 33 / 16;
+  // N = 32000, K = 1024, fp32 out: 100 rows 29 / 23, 512: 82 / 37; N = 1024, K = 4096, bf16 out (4 tiles): 100 rows 14 / 22, 256: 23 / 23,
+  // 384 (8): 25 / 24, 512: 33 / 23.
   const int64_t pair_tiles = (g.M + 255) / 256 * ((g.N + 255) / 256);
   if (g.N > 128 && g.M > 64 && (pair_tiles >= 16 || g.M > 384)) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
   const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
   const int64_t m_tiles = (g.M + nt - 1) / nt;
   // More tiles than a grid's y or z counts: the pairs walk over theirs in a loop.
   if (n_tiles > 65535 || m_tiles > 65535) return launch_many<OT>(g, A, a_stride, W, w_stride, sms, st);
-  // Ranks for two CTAs per SM. us with / without: N = 1024, K = 4096, 27 rows 16 / 23, 200 rows 26 / 37; N = 6144, K = 1536, 1 row 15 / 16.
+  // Ranks for two CTAs per SM. us (as above) with / without: N = 1024, K = 4096, 27 rows 10 / 21, 200 rows 21 / 31; N = 6144, K = 1536,
+  // 1 row 9.6 / 11.5.
   int ranks = 1;
   while (ranks < 8 && 2 * ranks <= kb && n_tiles * m_tiles * ranks * 2 <= 2 * sms) ranks *= 2;
   if (nt == 16) return launch_few<16, OT>(g, A, a_stride, W, w_stride, ranks, st);
@@ -147,7 +149,7 @@ int launch_gemm8(const g8::Args& g, const uint8_t* A, int64_t a_stride, const ui
 }
 
 // A block of up to 512 threads per row, two per SM; few rows of many ids: a cluster of blocks each, as long as all find room at once.
-// us with / without: 1 row of 131072 20 / 26, 8 rows 42 / 127, 32 rows of 60000 80 / 132.
+// us (events around a launch, L2 flushed before it) with / without: 1 row of 131072 29 / 36, 8 rows 48 / 139, 32 rows of 60000 94 / 135.
 template <typename T>
 int launch_sample(const smp::Args& p, cudaStream_t st) {
   int sms = 0;

@@ -45,7 +45,8 @@ __device__ __forceinline__ uint32_t logit_key(float l) {
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
 // A warp reads `E` logits per lane at a time, a stretch of 32 E consecutive ids: 16, or 4 where the ids are few (more threads then share
-// a row, and their maxima tell more of it). us with 16 / 4: 2000 rows of 1352 115 / 61, 4096 rows of 8000 181 / 200, 32 rows of 60000 80 / 185.
+// a row, and their maxima tell more of it). us (events around a launch, L2 flushed before it) with 16 / 4: 2000 rows of 1352 119 / 67, of
+// 4096 80 / 96 (the border lies between the two), 4096 rows of 8000 184 / 207.
 constexpr int kFewIds = 4096;
 constexpr int kMaxStretches = 512;               // 262144 ids
 constexpr int kMaxWarps = 32;
